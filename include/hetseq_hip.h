@@ -313,6 +313,40 @@ hs_status hs_normalize_adam_step(float* w, float* m, float* v, float* G, void* w
                                  double lr, double beta1, double beta2, double eps, double weight_decay, int64_t t,
                                  void* stream);
 
+/* ---- update of matrices by their orthogonalised momentum ---------------------------------------
+ * Beside hs_adam_step: weight matrices are updated as matrices.  A matrix of the flat buffers is given by where its first element is
+ * and how far apart its rows are (elements; ld == cols for a whole weight, whose offset hs_param_layout() reports).  A list may hold any
+ * shapes, 1 x 1 to 2^28 elements (sides rounded up to multiples of 64), wide or tall, but no element twice. */
+typedef struct {
+  int64_t offset, ld;
+  int32_t rows, cols;
+} hs_matrix;
+
+/* Bytes of scratch that hs_op_orthogonalize / hs_muon_step need for a list (0 for an invalid one).  Calls that overlap in time, and
+ * captured graphs that may, need a workspace each; nothing in it has to start at zero and nothing of it is kept for the next call. */
+size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_t products);
+
+/* y = orthogonalised x, matrix by matrix.  X = x / (|x|_F + eps) (zeros stay zeros), then `steps` times
+ * X <- a X + (b A + c A A) X with A = X X^T on the shorter side: an odd polynomial of the singular values, (a, b, c) =
+ * coeff[3 k .. 3 k + 2] in step k, or 3.4445, -4.7750, 2.0315 in all when coeff is NULL (five steps take singular values from
+ * 0.005 to 1 times the largest into 0.7 .. 1.2).
+ * dtype: element type of x and y (flat buffers of `size` elements, in which the list's matrices lie; y may be x; elements outside the matrices
+ * are not touched).  mats, coeff: host, copied.  products: HS_FP32 for products as exact as in fp32, HS_BF16 for 16-bit products with 32-bit
+ * sums (relative error about 1e-3 per matrix; both take any dtype).  The polynomials must keep the singular values below 3.9 and the
+ * entries of b A + c A A below 60 in size.  A matrix with a value that is not finite becomes NaN as a whole; the others do not see it. */
+hs_status hs_op_orthogonalize(int32_t dtype, const void* x, void* y, size_t size, const hs_matrix* mats, int32_t n, int32_t products,
+                              int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One update of the list's matrices.  g = G / denom (denom == 0: G), m = momentum m + g, u = g + momentum m (nesterov != 0) or m,
+ * w = (1 - lr weight_decay) w - lr s O(u) with O as in hs_op_orthogonalize and s = rms sqrt(max(rows, cols)), which makes the root
+ * mean square of the update rms times lr whatever the shape (rms > 0; 0.2 goes with learning rates made for Adam), or
+ * s = sqrt(max(1, rows / cols)) (rms == 0).
+ * w, m (in/out), G (in; unlike in hs_normalize_adam_step not written) flat fp32 [size] dev, w_lowp_out [size] dev bfloat16 or NULL as in hs_adam_step.  What
+ * lies outside the list's matrices is neither read nor written: update it with hs_normalize_adam_step. */
+hs_status hs_muon_step(float* w, float* m, const float* G, void* w_lowp_out, size_t size, const hs_matrix* mats, int32_t n,
+                       int32_t products, double denom, double lr, double momentum, int32_t nesterov, double weight_decay, double rms,
+                       int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The loss that a step reports (section "Optimizer and Learning Rate Scheduler": every worker's loss comes with a
  * weight, and the weighted sum over all workers divided by the global weight equals the non-distributed loss):
  * *loss_out = (loss_sums[0] + ... + loss_sums[n - 1]) / denom, the sums added in index order.  loss_sums [n] dev:
@@ -429,6 +463,26 @@ hs_status hs_op_gemm(int32_t dtype, int32_t a_kmajor, int32_t b_kmajor, int32_t 
                      const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
                      int32_t c_f32, float beta, const void* bias, int32_t epi, const void* aux,
                      int64_t ldaux, void* C2, void* scratch, size_t scratch_bytes, void* stream);
+
+/* ---- products in 8-bit floating point -----------------------------------------------------------
+ * Operands are codes of e4m3 (1 sign, 4 exponent, 3 significand bits, largest value 448, 0x7f NaN), one byte each, with one scale
+ * for every 128 of the contraction of every row: byte e stands for 2^(e - 127).  A row of K codes takes ceil(K / 128) whole blocks of
+ * 128 bytes, zeros behind the last code; its scales take a byte per block, in rows of whole 4-byte words.  Row strides are in bytes.
+ *
+ * hs_op_quantize_fp8 writes operands: x [R, C] (dtype, row stride ldx elements) as q [R, ldq], qs [R, ldqs] for contractions along its
+ * columns and, from the same read, transposed as qt [C, ldqt], qts [C, ldqts] for contractions along its rows (a pair may be NULL).  Scale: the
+ * smallest power of two with largest |value| <= 448 scale (at least 2^-127; 1 where all are zero), over 128 values (tile == 0: activations and their
+ * gradients) or over 128 x 128 (tile == 1: weights, whose two forms then hold the same values; every row repeats its tile's scale).  Codes are
+ * rounded to the nearest, ties to even.  A value that is not finite becomes NaN and does not count for the scale.  Scale bytes behind the last
+ * block are not written.  y = x W^T takes q of x and q of W; dx = dy W takes q of dy and qt of W; dW = dy^T x takes qt of dy and qt of x. */
+hs_status hs_op_quantize_fp8(int32_t dtype, const void* x, int64_t ldx, int32_t R, int32_t C, int32_t tile, void* q, int64_t ldq,
+                             uint8_t* qs, int64_t ldqs, void* qt, int64_t ldqt, uint8_t* qts, int64_t ldqts, void* stream);
+/* C[M,N] = sum_k A(m,k) B(n,k) of such operands, with 32-bit sums; C is float (c_f32 != 0; C = beta C + sum, beta == 0 does not read C) or
+ * bfloat16; bias [N] bfloat16 or NULL.  Row strides of codes multiples of 128 and at most 4 MiB, of scales multiples of 4.  scratch (dev, may
+ * be NULL) as in hs_op_gemm: with it, contractions of products with few tiles are split and the partial sums added in a fixed order. */
+hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, const uint8_t* as, int64_t ldas, const void* B,
+                         int64_t ldb, const uint8_t* bs, int64_t ldbs, void* C, int64_t ldc, int32_t c_f32, float beta,
+                         const void* bias, void* scratch, size_t scratch_bytes, void* stream);
 
 /* Timing aid, not part of the method: the library holds several tilings of its bf16 GEMM kernel (numbered 0 .. 11: block
  * tile, k-tile depth, blocks per CU, operands staged through registers or loaded into LDS directly, contraction split

@@ -41,6 +41,10 @@ class hs_ckpt_header(C.Structure):
                 ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double)]
 
 
+class hs_matrix(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("ld", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
+
+
 class HsError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS.get(status, status)}: {msg}")
@@ -66,6 +70,9 @@ _SIGNATURES = {
     "hs_grad_accum_normalize": (_I32, [_P, _P, _SZ, _I32, _D, _P]),
     "hs_adam_step": (_I32, [_P, _P, _P, _P, _P, _SZ, _D, _D, _D, _D, _D, _I64, _P]),
     "hs_normalize_adam_step": (_I32, [_P, _P, _P, _P, _P, _SZ, _D, _D, _D, _D, _D, _D, _I64, _P]),
+    "hs_orthogonalize_workspace_bytes": (_SZ, [_P, _I32, _I32]),
+    "hs_op_orthogonalize": (_I32, [_I32, _P, _P, _SZ, _P, _I32, _I32, _I32, _P, _D, _P, _SZ, _P]),
+    "hs_muon_step": (_I32, [_P, _P, _P, _P, _SZ, _P, _I32, _I32, _D, _D, _D, _I32, _D, _D, _I32, _P, _D, _P, _SZ, _P]),
     "hs_cast_params": (_I32, [_P, _P, _SZ, _I32, _P]),
     "hs_arm_update": (_I32, [_P, _P, _P, _P, _P, _P, _D, _D, _D, _D, _D, _D, _I64]),
     "hs_set_dropout": (_I32, [_P, _D, C.c_uint64, C.c_uint32]),
@@ -93,6 +100,8 @@ _SIGNATURES = {
     "hs_tune_gemm_variant": (_I32, [_I32]),
     "hs_gemm_choice": (_I32, [_I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _SZ, C.POINTER(_I32), C.POINTER(_I32)]),
     "hs_op_gemm": (_I32, [_I32, _I32, _I32, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _I32, _F, _P, _I32, _P, _I64, _P, _P, _SZ, _P]),
+    "hs_op_quantize_fp8": (_I32, [_I32, _P, _I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    "hs_op_gemm_fp8": (_I32, [_I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I32, _F, _P, _P, _SZ, _P]),
     "hs_op_layernorm_fwd": (_I32, [_I32, _P, _P, _P, _P, _P, _I32, _I32, _F, _P]),
     "hs_op_layernorm_bwd_scratch": (_SZ, [_I32, _I32]),
     "hs_op_layernorm_bwd": (_I32, [_I32, _P, _P, _P, _P, _P, _P, _P, _P, _F, _I32, _I32, _P, _P]),
@@ -354,6 +363,41 @@ def hs_normalize_adam_step(w, m, v, G, w_lowp_out, n, denom, lr, beta1, beta2, e
                                         weight_decay, t, _stream(stream)))
 
 
+def make_matrices(entries):
+    """The list (hs_matrix array) of (offset, ld, rows, cols) entries."""
+    return (hs_matrix * len(entries))(*[hs_matrix(int(o), int(ld), int(r), int(c)) for o, ld, r, c in entries])
+
+
+def hs_orthogonalize_workspace_bytes(mats, products) -> int:
+    n = int(lib().hs_orthogonalize_workspace_bytes(mats, len(mats), products))
+    if n == 0:
+        raise HsError(1, (lib().hs_last_error(None) or b"").decode())
+    return n
+
+
+def _coeff(coeff, steps):
+    """[steps, 3] coefficients as the host array that a call copies (None -> NULL)."""
+    if coeff is None:
+        return None
+    c = np.ascontiguousarray(coeff, dtype=np.float64)
+    if c.shape != (steps, 3):
+        raise HsError(1, f"coefficients of shape {c.shape}, not ({steps}, 3)")
+    return c
+
+
+def hs_op_orthogonalize(dtype, x, y, size, mats, products, steps, coeff, eps, workspace, workspace_bytes, stream=None):
+    c = _coeff(coeff, steps)
+    _check(lib().hs_op_orthogonalize(dtype, _ptr(x), _ptr(y), size, mats, len(mats), products, steps, _ptr(c), eps, _ptr(workspace), workspace_bytes,
+                                     _stream(stream)))
+
+
+def hs_muon_step(w, m, G, w_lowp_out, size, mats, products, denom, lr, momentum, nesterov, weight_decay, rms, steps, coeff, eps, workspace,
+                 workspace_bytes, stream=None):
+    c = _coeff(coeff, steps)
+    _check(lib().hs_muon_step(_ptr(w), _ptr(m), _ptr(G), _ptr(w_lowp_out), size, mats, len(mats), products, denom, lr, momentum, nesterov, weight_decay,
+                              rms, steps, _ptr(c), eps, _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
 def hs_cast_params(src, dst, n, dst_dtype, stream=None):
     _check(lib().hs_cast_params(_ptr(src), _ptr(dst), n, dst_dtype, _stream(stream)))
 
@@ -375,6 +419,16 @@ def hs_op_gemm(dtype, a_kmajor, b_kmajor, M, N, K, A, lda, B, ldb, Cm, ldc, c_f3
                ldaux=0, C2=None, scratch=None, scratch_bytes=0, stream=None):
     _check(lib().hs_op_gemm(dtype, a_kmajor, b_kmajor, M, N, K, _ptr(A), lda, _ptr(B), ldb, _ptr(Cm), ldc, c_f32, beta,
                             _ptr(bias), epi, _ptr(aux), ldaux, _ptr(C2), _ptr(scratch), scratch_bytes, _stream(stream)))
+
+
+def hs_op_quantize_fp8(dtype, x, ldx, R, C, tile, q, ldq, qs, ldqs, qt=None, ldqt=0, qts=None, ldqts=0, stream=None):
+    _check(lib().hs_op_quantize_fp8(dtype, _ptr(x), ldx, R, C, tile, _ptr(q), ldq, _ptr(qs), ldqs, _ptr(qt), ldqt, _ptr(qts), ldqts, _stream(stream)))
+
+
+def hs_op_gemm_fp8(M, N, K, A, lda, a_scale, ldas, B, ldb, b_scale, ldbs, Cm, ldc, c_f32=0, beta=0.0, bias=None, scratch=None, scratch_bytes=0,
+                   stream=None):
+    _check(lib().hs_op_gemm_fp8(M, N, K, _ptr(A), lda, _ptr(a_scale), ldas, _ptr(B), ldb, _ptr(b_scale), ldbs, _ptr(Cm), ldc, c_f32, beta, _ptr(bias),
+                                _ptr(scratch), scratch_bytes, _stream(stream)))
 
 
 def hs_gemm_choice(a_kmajor, b_kmajor, M, N, K, c_f32=0, epi=0, a_padded=0, scratch_bytes=0):

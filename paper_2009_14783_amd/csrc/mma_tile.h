@@ -1,0 +1,169 @@
+// Main loop of a block tile for products whose operands are not bf16: 16-bit floats (fp16), and 8-bit codes with a scale for every 128 of the
+// contraction.  A row of a k-tile is 128 bytes in both, so that the operand tiles, their LDS layout and the ring of stages are those of gemm_dma.h; only
+// the matrix instruction and the bytes that a lane feeds to it differ.
+#pragma once
+#include "gemm_dma.h"
+
+namespace {
+
+typedef _Float16 f16;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// fp16: a slice of a k-tile is 16 deep, a lane holds the 8 elements at 8 (lane / 32) of it
+struct MmaF16 {
+  typedef f16x8 Frag;                // as it is read from LDS
+  typedef f16x8 Op;                  // as it is multiplied
+  static constexpr int KS = 4;       // slices of a k-tile
+  template <class T>
+  static __device__ __forceinline__ Frag frag(const bf16* __restrict__ s, int rbase, int ks, int lane) {
+    union { bf16x8 b; f16x8 h; } u;
+    u.b = T::frag(s, rbase, ks, lane);
+    return u.h;
+  }
+  static __device__ __forceinline__ Op op(const Frag& f, int) { return f; }
+  static __device__ __forceinline__ void mma(const Op& a, const Op& b, f32x16& c, int, int) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+// 8-bit codes at the 8-bit rate: a slice is 64 deep, a lane holds 32 codes of its row and the instruction multiplies them by 2^(byte 0 of the scale -
+// 127).  Which of the 64 it holds does not matter as long as both operands agree, since the whole k-tile has one scale: it takes the two 16-byte chunks
+// that a lane takes in two slices of 16-bit elements.
+// The instruction adds products in groups of 8 neighbours that it aligns to the largest of them and cuts 13 bits below its leading one (measured: 448 * 448 - 448 * 448 + 2
+// is 0 within 8 neighbours and 2 otherwise), in 32 bits from there on: 1.4e-5 relative to a Gaussian product, up to 4e-5 with rows of different size.
+// That is a hundredth of the rounding of a bf16 result, but not what a 32-bit one may lose: see MmaE4M3Wide.
+struct MmaE4M3 {
+  typedef i32x8 Frag;
+  typedef i32x8 Op;
+  static constexpr int KS = 2;
+  template <class T>
+  static __device__ __forceinline__ Frag frag(const bf16* __restrict__ s, int rbase, int ks, int lane) {
+    union { bf16x8 b[2]; i32x8 v; } u;
+    u.b[0] = T::frag(s, rbase, 2 * ks, lane);
+    u.b[1] = T::frag(s, rbase, 2 * ks + 1, lane);
+    return u.v;
+  }
+  static __device__ __forceinline__ int scale(uint32_t word, int t) { return (int)(word >> (8 * (t & 3))); }
+  static __device__ __forceinline__ Op op(const Frag& f, int) { return f; }
+  static __device__ __forceinline__ void mma(const Op& a, const Op& b, f32x16& c, int sa, int sb) {
+    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
+  }
+};
+// 8-bit codes for 32-bit results: a lane's 16 codes of a 32-deep slice become bf16 with their scale (both exact: 4 significant bits, 8 of exponent) and
+// go through two bf16 instructions, whose sums are 32 bits throughout.  Half the rate of MmaE4M3.
+struct MmaE4M3Wide {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  typedef i32x4 Frag;
+  struct Op { bf16x8 v[2]; };
+  static constexpr int KS = 4;
+  template <class T>
+  static __device__ __forceinline__ Frag frag(const bf16* __restrict__ s, int rbase, int ks, int lane) {
+    union { bf16x8 b; i32x4 v; } u;
+    u.b = T::frag(s, rbase, ks, lane);
+    return u.v;
+  }
+  // the scale as a float: 2^(byte - 127)
+  static __device__ __forceinline__ int scale(uint32_t word, int t) { return (int)((word >> (8 * (t & 3)) & 0xffu) << 23); }
+  static __device__ __forceinline__ Op op(const Frag& f, int s) {
+    typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    union { bf16x2 p[8]; Op o; } u;
+    const float x = __int_as_float(s);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      u.p[2 * k] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[k], x, false);
+      u.p[2 * k + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[k], x, true);
+    }
+    return u.o;
+  }
+  static __device__ __forceinline__ void mma(const Op& a, const Op& b, f32x16& c, int, int) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v[0], b.v[0], c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v[1], b.v[1], c, 0, 0, 0);
+  }
+};
+
+// The pipeline of ahead_step over `nk` k-tiles: fragments are read one slice ahead, the barrier sits before the last slice of a k-tile.
+// next(dst): requests the next k-tile into the stage at dst; it is called S times more than there are k-tiles to be used, and what it requests beyond
+// them has to be harmless (an offset behind the operand, where a load returns zeros).  scales(t): called when k-tile t is about to be used and
+// its loads have landed; sa and sb are the scale registers of the tile's fragments (unused by fp16).
+template <class C, class MMA, class TA, class TB, class Next, class Scales>
+__device__ __forceinline__ void mma_loop(int nk, unsigned char* lds_raw, f32x16 (&acc)[C::TI][C::TJ], int (&sa)[C::TI], int (&sb)[C::TJ], int wm, int wn,
+                                         int lane, Next&& next, Scales&& scales) {
+  constexpr int TI = C::TI, TJ = C::TJ, S = C::S, KS = MMA::KS, NM = TI * TJ, NL = TA::NI + TB::NI;
+  constexpr int NF = TI + TJ, FPM = (NF + NM - 1) / NM, RPS = sizeof(typename MMA::Frag) / 16;      // LDS reads per k-major fragment
+  static_assert(KS % 2 == 0, "fragment sets alternate");
+  typename MMA::Frag fa[2][TI], fb[2][TJ];
+  auto read = [&](int set, const unsigned char* st, int ks) __attribute__((always_inline)) {
+    const bf16* sA = (const bf16*)st;
+    const bf16* sB = (const bf16*)(st + TA::BYTES);
+#pragma unroll
+    for (int i = 0; i < TI; ++i) fa[set][i] = MMA::template frag<TA>(sA, (wm * TI + i) * 32, ks, lane);
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) fb[set][j] = MMA::template frag<TB>(sB, (wn * TJ + j) * 32, ks, lane);
+  };
+#pragma unroll
+  for (int s = 0; s < S; ++s) next(lds_raw + s * C::STAGE);
+  asm volatile("" ::: "memory");
+  wait_loads<(S - 1) * NL>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read(0, lds_raw, 0);
+  scales(0);
+  for (int t0 = 0; t0 < nk; t0 += S) {
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+      const int t = t0 + u;
+      if (t >= nk) break;
+      unsigned char* const cur = lds_raw + u * C::STAGE;
+      const unsigned char* const nxt = lds_raw + ((u + 1) % S) * C::STAGE;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int fc = s & 1, fn = fc ^ 1;
+        const bool last = s == KS - 1;
+        if (last) {
+          asm volatile("" ::: "memory");
+          wait_loads<(S - 2) * NL>();
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+        }
+        read(fn, last ? nxt : (const unsigned char*)cur, last ? 0 : s + 1);
+        if (last) next(cur);
+        typename MMA::Op oa[TI], ob[TJ];
+#pragma unroll
+        for (int i = 0; i < TI; ++i) oa[i] = MMA::op(fa[fc][i], sa[i]);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) ob[j] = MMA::op(fb[fc][j], sb[j]);
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+          for (int j = 0; j < TJ; ++j) MMA::mma(oa[i], ob[j], acc[i][j], sa[i], sb[j]);
+#pragma unroll
+        for (int q = 0; q < NM; ++q) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                       // MFMA
+#pragma unroll
+          for (int f = q * FPM; f < (q + 1) * FPM && f < NF; ++f) {                                // fragment reads of the next slice
+            if (f < TI) __builtin_amdgcn_sched_group_barrier(0x100, TA::RPF * RPS, 0);
+            else __builtin_amdgcn_sched_group_barrier(0x100, TB::RPF * RPS, 0);
+          }
+          if (last) __builtin_amdgcn_sched_group_barrier(0x020, (NL + NM - 1) / NM, 0);            // loads
+        }
+      }
+      scales(t + 1);
+    }
+  }
+  asm volatile("" ::: "memory");
+  wait_loads<0>();
+  __builtin_amdgcn_s_barrier();      // every wave is done with the stages, and nothing is in flight to them
+  asm volatile("" ::: "memory");
+}
+
+template <int TI, int TJ>
+__device__ __forceinline__ void clear_tiles(f32x16 (&acc)[TI][TJ]) {
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+}
+
+}  // namespace

@@ -14,6 +14,42 @@ import torch
 from . import binding as hs
 
 
+class MatrixUpdate:
+    """Which parameters hs_muon_step updates and which are left to Adam: the weights of the layers and of the masked-LM head's transform as matrices (of
+    the fused query/key/value projections every H x H block by itself), embeddings, biases and LayerNorm parameters by Adam.  The momentum of a matrix
+    is its slice of the worker's first moment, so that a checkpoint holds it."""
+
+    DEFAULTS = dict(momentum=0.95, nesterov=True, weight_decay=0.0, rms=0.2, steps=5, coeff=None, eps=1e-7)
+
+    def __init__(self, layout, hidden: int, compute: int, device):
+        self.products, whole, end = compute, [], 0
+        self.ranges = []           # (first parameter, number of parameters) between the matrices
+        for name, off, rows, cols in layout:
+            if not name.endswith(".w"):
+                continue
+            if off > end:
+                self.ranges.append((end, off - end))
+            end = off + rows * cols
+            n = rows // hidden if name.endswith(("qkv.w", "ckv.w")) else 1
+            whole += [(off + i * (rows // n) * cols, cols, rows // n, cols) for i in range(n)]
+        total = max(off + r * c for _, off, r, c in layout)
+        if total > end:
+            self.ranges.append((end, total - end))
+        self.mats = hs.make_matrices(whole)
+        self.bytes = hs.hs_orthogonalize_workspace_bytes(self.mats, self.products)
+        self.ws = torch.empty(self.bytes, dtype=torch.uint8, device=device)
+
+    def apply(self, worker, denom: float, adam: dict, muon: dict, t: int):
+        """Update number t of all parameters with the gradient sums in worker.G.  Adam's share of G is divided by denom in place; the matrices' share stays."""
+        o = dict(self.DEFAULTS, **muon)
+        hs.hs_muon_step(worker.w, worker.m, worker.G, worker.w_lowp, worker.P, self.mats, self.products, denom, o.get("lr", adam["lr"]), o["momentum"],
+                        1 if o["nesterov"] else 0, o["weight_decay"], o["rms"], o["steps"], o["coeff"], o["eps"], self.ws, self.bytes)
+        for off, n in self.ranges:
+            w, m, v, G = (t[off:off + n] for t in (worker.w, worker.m, worker.v, worker.G))
+            low = None if worker.w_lowp is None else worker.w_lowp[off:off + n]
+            hs.hs_normalize_adam_step(w, m, v, G, low, n, denom, adam["lr"], adam["beta1"], adam["beta2"], adam["eps"], adam.get("weight_decay", 0.0), t)
+
+
 class Worker:
     def __init__(self, model: dict, compute: str, theta0: np.ndarray, device: str = "cuda:0"):
         self.device = torch.device(device)
@@ -37,6 +73,7 @@ class Worker:
         else:
             self.w_lowp = None
         self.t = 0
+        self._matrices = None
         self._drop_on = False
         self._acts = self._ws = self._hidden = self._dhidden = None
         self._acts_bytes = self._ws_bytes = 0
@@ -147,12 +184,27 @@ class Worker:
             hs.hs_fill_zero(self.G, 4 * self.P)
         return n_total
 
-    def train_step(self, batches: list, adam: dict, denom=None, fused: bool = True, update_in_backward: bool = True):
+    @property
+    def matrices(self) -> MatrixUpdate:
+        """The plan of updates with `muon`, made on first use."""
+        if self._matrices is None:
+            self._matrices = MatrixUpdate(hs.hs_param_layout(self.cfg), self.H, self.compute, self.device)
+        return self._matrices
+
+    def train_step(self, batches: list, adam: dict, denom=None, fused: bool = True, update_in_backward: bool = True, muon: dict = None):
         """The whole hot path for one optimizer step.  Returns the sample count D; the loss sums
         stay on the device in loss_buf (read with reported_loss after synchronising).
         update_in_backward (fused accumulation only): normalisation and Adam are armed for the last
         micro-batch's backward pass, which applies them per parameter group as soon as that group's
-        gradient is final (same arithmetic, same bits as the two separate calls)."""
+        gradient is final (same arithmetic, same bits as the two separate calls).
+        muon: weight matrices are updated by their orthogonalised momentum behind the backward pass (hs_muon_step), the other
+        parameters by Adam; a dict of the arguments of MatrixUpdate.DEFAULTS that are to differ, and "lr" (adam's if absent)."""
+        if muon is not None:
+            n_total = self.accumulate_micro_batches(batches, fused)
+            D = n_total if denom is None else denom
+            self.matrices.apply(self, float(D), adam, muon, self.t + 1)
+            self.t += 1
+            return D
         real = [d for d in batches if d is not None and not d.get("dummy", False)]
         D = sum(d["n_seq"] for d in real) if denom is None else denom
         wd = adam.get("weight_decay", 0.0)
@@ -175,16 +227,16 @@ class Worker:
         return float(self.loss_out[0].item())
 
     # ---- multi-step loop: schedule and checkpoints (call order only, like the rest of this class) ----
-    def train(self, n_steps: int, micro_batches_of, adam: dict, schedule: dict) -> list:
+    def train(self, n_steps: int, micro_batches_of, adam: dict, schedule: dict, muon: dict = None) -> list:
         """n_steps updates; update number t = completed updates + 1 takes its micro-batches (host dicts)
         from micro_batches_of(t) and its learning rate from hs_lr_linear(t, **schedule).  Returns the
-        reported loss of every update."""
+        reported loss of every update.  muon as in train_step."""
         losses = []
         for _ in range(n_steps):
             t = self.t + 1
             lr = hs.hs_lr_linear(t, schedule["max_lr"], schedule["warmup"], schedule["total"])
             batches = [None if (mb is None or mb.get("dummy", False)) else self.upload(mb) for mb in micro_batches_of(t)]
-            D = self.train_step(batches, dict(adam, lr=lr))
+            D = self.train_step(batches, dict(adam, lr=lr), muon=muon)
             losses.append(self.reported_loss(D))
         return losses
 
@@ -242,6 +294,7 @@ class PairWorker:
             self.w_lowp = torch.empty(self.P, dtype=torch.bfloat16, device=dev)
             hs.hs_cast_params(self.w, self.w_lowp, self.P, hs.HS_BF16)
         self.t = 0
+        self._matrices = None
         self._drop_on = False
         self._acts = self._ws = self._out = self._dout = None
         self._acts_bytes = self._ws_bytes = 0
@@ -309,20 +362,29 @@ class PairWorker:
             if packed:
                 hs.hs_s2s_set_lengths(self.ctx, None, None)
 
-    def train_step(self, batches: list, adam: dict, denom=None, update_in_backward=None):
+    @property
+    def matrices(self) -> MatrixUpdate:
+        """The plan of updates with `muon`, made on first use."""
+        if self._matrices is None:
+            self._matrices = MatrixUpdate(hs.hs_s2s_param_layout(self.cfg), self.H, self.compute, self.device)
+        return self._matrices
+
+    def train_step(self, batches: list, adam: dict, denom=None, update_in_backward=None, muon: dict = None):
         """One optimizer step over the uploaded micro-batches (None = a pass without data).  Returns the weight D used
         (the number of real target tokens by default).  update_in_backward True: normalisation and Adam are armed for the last
         micro-batch's backward pass, which applies them layer by layer as soon as a layer's gradient is final (same
         arithmetic, same bits as the separate call).  False: the separate call behind the pass, so that a backward pass that fails leaves the
         weights as they were.  None (default): armed from 4 M parameters on: below, the launches per layer
         cost more than the one update behind the pass (toy model 0.602 -> 0.610 ms per step); above, the update of 0.43 ms runs beside
-        the pass (ms per step of the base model: 320 rows per side 2.15 -> 1.96, 4096 4.18 -> 4.08, 8064 6.71 -> 6.65)."""
+        the pass (ms per step of the base model: 320 rows per side 2.15 -> 1.96, 4096 4.18 -> 4.08, 8064 6.71 -> 6.65).  muon: as in Worker.train_step; the update
+        is then behind the pass."""
         assert len(batches) <= 64
         hs.hs_fill_zero(self.loss_buf, 4 * self.loss_buf.numel())
         real = [i for i, d in enumerate(batches) if d is not None]
         D = float(denom if denom is not None else max(sum(batches[i]["n_tok"] for i in real), 1))
         self.t += 1
         first, in_backward = True, self.P >= 4 << 20 if update_in_backward is None else update_in_backward
+        in_backward = in_backward and muon is None
         arm = lambda: hs.hs_arm_update(self.ctx, self.w, self.m, self.v, self.G, self.w_lowp, D, adam["lr"], adam["beta1"], adam["beta2"],
                                        adam["eps"], adam.get("weight_decay", 0.0), self.t)
         for i, d in enumerate(batches):
@@ -333,7 +395,9 @@ class PairWorker:
             first = False
         if first:
             hs.hs_fill_zero(self.G, 4 * self.P)
-        if first or not in_backward:
+        if muon is not None:
+            self.matrices.apply(self, D, adam, muon, self.t)
+        elif first or not in_backward:
             hs.hs_normalize_adam_step(self.w, self.m, self.v, self.G, self.w_lowp, self.P, D, adam["lr"], adam["beta1"], adam["beta2"],
                                       adam["eps"], adam.get("weight_decay", 0.0), self.t)
         return D

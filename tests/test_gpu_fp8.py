@@ -1,0 +1,296 @@
+"""The 8-bit products and their quantiser on a GPU against the 64-bit oracle."""
+import numpy as np
+import pytest
+
+from oracle import matrix_ops as M
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hs():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2009_14783_amd import binding
+    binding.lib()            # a missing library is a failure, not a skip
+    return binding
+
+
+FILL = 0xA5
+
+
+def wide(n):
+    return -(-n // 128) * 128
+
+
+def words(n):
+    return -(-(-(-n // 128)) // 4) * 4
+
+
+def buffers(rows, n, extra=0):
+    """Codes and scales for `rows` rows of n, filled with a pattern; `extra` more blocks per row and rows behind the last."""
+    q = torch.full((rows + 1, wide(n) + 128 * extra), FILL, dtype=torch.uint8, device="cuda")
+    s = torch.full((rows + 1, words(n) + 4 * extra), FILL, dtype=torch.uint8, device="cuda")
+    return q, s
+
+
+def quantize(hs, x, dtype, tile, both=(True, True), extra=0, ldx=None):
+    R, C = x.shape
+    ldx = C if ldx is None else ldx
+    q, s = buffers(R, C, extra)
+    qt, st = buffers(C, R, extra)
+    a = (q, q.shape[1], s, s.shape[1]) if both[0] else (None, 0, None, 0)
+    b = (qt, qt.shape[1], st, st.shape[1]) if both[1] else (None, 0, None, 0)
+    hs.hs_op_quantize_fp8(dtype, x, ldx, R, C, int(tile), *a, *b)
+    torch.cuda.synchronize()
+    return [t.cpu().numpy() for t in (q, s, qt, st)]
+
+
+def check_codes(q, s, want_q, want_s, rows, n):
+    kb = -(-n // 128)
+    assert np.array_equal(s[:rows, :kb], want_s) and np.array_equal(q[:rows, :wide(n)], want_q)
+    assert np.all(s[:rows, kb:] == FILL) and np.all(q[:rows, wide(n):] == FILL) and np.all(q[rows:] == FILL) and np.all(s[rows:] == FILL)
+
+
+@pytest.mark.parametrize("R,C", [(1, 1), (1, 200), (200, 1), (37, 200), (128, 128), (129, 127), (300, 520), (64, 1000)])
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("tile", [False, True])
+def test_quantiser_bit_for_bit(hs, R, C, dtype, tile):
+    rng = np.random.default_rng(R * 1000 + C)
+    x = torch.from_numpy((rng.standard_normal((R, C)) * np.exp(2 * rng.standard_normal((R, 1)))).astype(np.float32)).to(torch.bfloat16 if dtype else torch.float32)
+    h = x.double().numpy()
+    q, s, qt, st = quantize(hs, x.cuda(), dtype, tile, extra=1)
+    check_codes(q, s, *M.quantize(h, tile), R, C)
+    check_codes(qt, st, *M.quantize(h.T, tile), C, R)
+
+
+@pytest.mark.parametrize("both", [(True, False), (False, True)])
+@pytest.mark.parametrize("tile", [False, True])
+def test_one_form_alone_and_rows_inside_a_wider_matrix(hs, both, tile):
+    rng = np.random.default_rng(8)
+    big = torch.from_numpy(rng.standard_normal((150, 411)).astype(np.float32)).cuda()
+    for first in (0, 3, 8):
+        x = big[:, first:first + 300]
+        R, C = x.shape
+        q, s = buffers(R, C)
+        qt, st = buffers(C, R)
+        a = (q, q.shape[1], s, s.shape[1]) if both[0] else (None, 0, None, 0)
+        b = (qt, qt.shape[1], st, st.shape[1]) if both[1] else (None, 0, None, 0)
+        hs.hs_op_quantize_fp8(0, x, 411, R, C, int(tile), *a, *b)
+        torch.cuda.synchronize()
+        h = x.cpu().double().numpy()
+        if both[0]:
+            check_codes(q.cpu().numpy(), s.cpu().numpy(), *M.quantize(h, tile), R, C)
+        if both[1]:
+            check_codes(qt.cpu().numpy(), st.cpu().numpy(), *M.quantize(h.T, tile), C, R)
+
+
+def test_values_at_the_borders(hs):
+    """Ties, the limits of a scale, zeros, subnormals, the largest values, infinities and NaN."""
+    grid = M.e4m3_value(np.arange(127))
+    ties = (grid[1:] + grid[:-1]) / 2
+    rows = np.zeros((12, 256))
+    rows[0, :127], rows[1, :126], rows[2, :126] = grid, ties, -np.nextafter(ties, 1e9)
+    rows[0, 127] = rows[1, 127] = rows[2, 127] = 448
+    rows[3, 0], rows[4, 0], rows[5, 0] = 448 * 2.0 ** 30, np.nextafter(np.float32(448 * 2.0 ** 30), np.float32(np.inf)), 2.0 ** -140
+    rows[6, :3], rows[7, :3] = (3.4e38, -1e38, 1e30), (1e-38, -3e-39, 1e-45)
+    rows[8, :4], rows[9, 5], rows[10, 200] = (np.inf, 1.0, -2.5, 3.0), np.nan, -np.inf
+    x = rows.astype(np.float32)
+    q, s, qt, st = quantize(hs, torch.from_numpy(x).cuda(), 0, False)
+    h = x.astype(np.float64)
+    for got, gs, want in ((q, s, h), (qt, st, h.T)):
+        wq, ws = M.quantize(want)
+        n = want.shape[0]
+        assert np.array_equal(gs[:n, :ws.shape[1]], ws)
+        nan = (wq & 0x7f) == 0x7f
+        assert np.array_equal((got[:n] & 0x7f) == 0x7f, nan) and np.array_equal(got[:n][~nan], wq[~nan])
+
+
+def operand(rng, rows, K, spread):
+    """Random codes (no NaN) and scales of rows x K, as stored, with other bytes where nothing is read."""
+    q = rng.integers(0, 256, (rows, wide(K)), dtype=np.uint8)
+    q[(q & 0x7f) == 0x7f] = 0x30
+    q[:, K:] = 0
+    s = np.full((rows, words(K)), 0xff, dtype=np.uint8)
+    s[:, :-(-K // 128)] = rng.integers(127 - spread, 128 + spread, (rows, -(-K // 128)), dtype=np.uint8)
+    return q, s
+
+
+def dev(*arrays):
+    return [torch.from_numpy(a).cuda() for a in arrays]
+
+
+def product(hs, M_, N, K, a, sa, b, sb, c, ldc, **kw):
+    hs.hs_op_gemm_fp8(M_, N, K, a, a.shape[1], sa, sa.shape[1], b, b.shape[1], sb, sb.shape[1], c, ldc, **kw)
+    torch.cuda.synchronize()
+
+
+SHAPES = [(1, 1, 1), (1, 700, 1024), (3, 33, 128), (16, 257, 4224), (37, 53, 200), (64, 64, 129), (65, 129, 640), (128, 128, 512), (130, 300, 1000), (257, 513, 300),
+          (1000, 1100, 640), (1500, 2100, 256), (2048, 4096, 384), (129, 96, 9000), (4099, 8, 130), (8, 4099, 130)]
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("scratch", [0, 32 << 20])
+def test_product_against_the_oracle(hs, m, n, k, scratch):
+    """fp32 results: the sum in another order, K + 2 roundings of 2^-24 of the sum of the products' sizes at most.  bf16: 2^-8 of the value, and what the 8-bit
+    instruction drops: the adder of 8 neighbours cuts 13 bits below the leading one of the largest, so at most 8 units of 2^-12 of that product
+    (two's complement, cut towards minus infinity), 2^-9 of the sum of sizes."""
+    rng = np.random.default_rng(m * 7 + n * 3 + k)
+    a, sa = operand(rng, m, k, 3)
+    b, sb = operand(rng, n, k, 3)
+    bias = torch.from_numpy(rng.standard_normal(n).astype(np.float32) * 1e4).to(torch.bfloat16)
+    da, dsa, db, dsb = dev(a, sa, b, sb)
+    ws = torch.empty(scratch, dtype=torch.uint8, device="cuda") if scratch else None
+    kw = dict(scratch=ws, scratch_bytes=scratch)
+    c = torch.full((m + 1, n + 3), 7.5, device="cuda")
+    product(hs, m, n, k, da, dsa, db, dsb, c, n + 3, c_f32=1, **kw)
+    want, size = M.gemm_fp8(a, sa, b, sb, k)
+    got = c.cpu().double().numpy()
+    assert np.all(np.abs(got[:m, :n] - want) <= (k + 2) * 2.0 ** -24 * size + 1e-30)
+    assert np.all(got[m] == 7.5) and np.all(got[:, n:] == 7.5)
+    # beta and bias on top of what is there
+    product(hs, m, n, k, da, dsa, db, dsb, c, n + 3, c_f32=1, beta=-0.5, bias=bias.cuda(), **kw)
+    want2, size2 = M.gemm_fp8(a, sa, b, sb, k, bias.double().numpy(), got[:m, :n], -0.5)
+    assert np.all(np.abs(c.cpu().double().numpy()[:m, :n] - want2) <= (k + 4) * 2.0 ** -24 * size2 + 1e-30)
+    o = torch.full((m + 1, n + 5), 7.5, dtype=torch.bfloat16, device="cuda")
+    product(hs, m, n, k, da, dsa, db, dsb, o, n + 5, bias=bias.cuda(), **kw)
+    want, size = M.gemm_fp8(a, sa, b, sb, k, bias.double().numpy())
+    got = o.cpu().double().numpy()
+    bound = 2.0 ** -8 * np.abs(want) + 1.01 * (2.0 ** -9 + (k + 2) * 2.0 ** -24) * size
+    assert np.all(np.abs(got[:m, :n] - want) <= bound + 1e-30)
+    # over all elements the rounding of a value is 2^-8 / sqrt(3) and less; what is dropped is far below (random signs)
+    assert np.linalg.norm(got[:m, :n] - want) <= 2.0 ** -8 * np.linalg.norm(want) + 2.0 ** -12 * np.linalg.norm(size) / np.sqrt(k)
+    assert np.all(got[m] == 7.5) and np.all(got[:, n:] == 7.5)
+
+
+def test_contraction_of_length_zero(hs):
+    c = torch.full((3, 5), 2.0, device="cuda")
+    bias = torch.arange(5, device="cuda").to(torch.bfloat16)
+    hs.hs_op_gemm_fp8(3, 5, 0, None, 128, None, 4, None, 128, None, 4, c, 5, c_f32=1, beta=0.5, bias=bias)
+    torch.cuda.synchronize()
+    assert torch.equal(c.cpu(), (1.0 + torch.arange(5.0)).expand(3, 5))
+    o = torch.full((3, 5), 2.0, dtype=torch.bfloat16, device="cuda")
+    hs.hs_op_gemm_fp8(3, 5, 0, None, 128, None, 4, None, 128, None, 4, o, 5)
+    torch.cuda.synchronize()
+    assert torch.all(o == 0)
+
+
+def test_nan_codes_and_scales_stay_in_their_rows(hs):
+    rng = np.random.default_rng(4)
+    m, n, k = 70, 90, 300
+    a, sa = operand(rng, m, k, 1)
+    b, sb = operand(rng, n, k, 1)
+    a[5, 17], b[40, 299], sa[9, 1] = 0x7f, 0xff, 0xff
+    c = torch.empty(m, n, device="cuda")
+    o = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    da, dsa, db, dsb = dev(a, sa, b, sb)
+    product(hs, m, n, k, da, dsa, db, dsb, c, n, c_f32=1)
+    product(hs, m, n, k, da, dsa, db, dsb, o, n)
+    want = np.zeros((m, n), bool)
+    want[5], want[:, 40], want[9] = True, True, True
+    for t in (c, o):
+        assert np.array_equal(~np.isfinite(t.cpu().float().numpy()), want)
+
+
+@pytest.mark.parametrize("e", [-60, 0, 55])
+def test_scales_far_from_one(hs, e):
+    rng = np.random.default_rng(12)
+    a, sa = operand(rng, 40, 256, 2)
+    b, sb = operand(rng, 50, 256, 2)
+    sa[:, :2] = (sa[:, :2].astype(int) + e).astype(np.uint8)
+    c = torch.empty(40, 50, device="cuda")
+    da, dsa, db, dsb = dev(a, sa, b, sb)
+    product(hs, 40, 50, 256, da, dsa, db, dsb, c, 50, c_f32=1)
+    want, size = M.gemm_fp8(a, sa, b, sb, 256)
+    assert np.all(np.abs(c.cpu().double().numpy() - want) <= 258 * 2.0 ** -24 * size)
+
+
+def test_rows_with_room_between_them(hs):
+    rng = np.random.default_rng(2)
+    m, n, k = 100, 140, 300
+    a, sa = operand(rng, m, k, 2)
+    b, sb = operand(rng, n, k, 2)
+    want, size = M.gemm_fp8(a, sa, b, sb, k)
+    pad = lambda t, w: np.concatenate([t, np.full((t.shape[0], w), 0x7f, np.uint8)], 1)
+    da, dsa, db, dsb = dev(pad(a, 256), pad(sa, 8), pad(b, 128), pad(sb, 4))
+    c = torch.empty(m, n, device="cuda")
+    product(hs, m, n, k, da, dsa, db, dsb, c, n, c_f32=1)
+    assert np.all(np.abs(c.cpu().double().numpy() - want) <= (k + 2) * 2.0 ** -24 * size)
+
+
+def test_layer_forward_and_backward_through_8_bits(hs):
+    """y = x W^T + b, dx = dy W and dW += dy^T x with everything quantised by the library, against the same in 64 bits."""
+    rng = np.random.default_rng(21)
+    T, K, N = 333, 200, 300
+    bf = lambda a: torch.from_numpy(a.astype(np.float32)).to(torch.bfloat16)
+    x, w, dy, bias = bf(rng.standard_normal((T, K))), bf(0.02 * rng.standard_normal((N, K))), bf(1e-3 * rng.standard_normal((T, N))), bf(rng.standard_normal(N))
+    old = rng.standard_normal((N, K)).astype(np.float32)
+    forms = {}
+    for name, t, tile in (("x", x, 0), ("w", w, 1), ("dy", dy, 0)):
+        R, C = t.shape
+        q, s = buffers(R, C)
+        qt, st = buffers(C, R)
+        hs.hs_op_quantize_fp8(1, t.cuda(), C, R, C, tile, q, q.shape[1], s, s.shape[1], qt, qt.shape[1], st, st.shape[1])
+        forms[name] = (q, s, qt, st)
+    y, dx, dw = (torch.empty(T, n, dtype=torch.bfloat16, device="cuda") for n in (N, K, 1))
+    dw = torch.from_numpy(old.copy()).cuda()
+    X, W, D = forms["x"], forms["w"], forms["dy"]
+    product(hs, T, N, K, X[0], X[1], W[0], W[1], y, N, bias=bias.cuda())
+    product(hs, T, K, N, D[0], D[1], W[2], W[3], dx, K)
+    product(hs, N, K, T, D[2], D[3], X[2], X[3], dw, K, c_f32=1, beta=1.0)
+    h = {k: v.double().numpy() for k, v in (("x", x), ("w", w), ("dy", dy), ("b", bias))}
+    xq, wq, dq = M.quantize(h["x"]), M.quantize(h["w"], True), M.quantize(h["dy"])
+    wtq, xtq, dtq = M.quantize(h["w"].T, True), M.quantize(h["x"].T), M.quantize(h["dy"].T)
+    for got, (want, size), k, bits in ((y, M.gemm_fp8(*xq, *wq, K, h["b"]), K, 8), (dx, M.gemm_fp8(*dq, *wtq, N), N, 8), (dw, M.gemm_fp8(*dtq, *xtq, T, None, old.astype(np.float64), 1.0), T, 24)):
+        err = np.abs(got.cpu().double().numpy() - want)
+        assert np.all(err <= 2.0 ** -bits * np.abs(want) + ((2.0 ** -9 if bits == 8 else 0.0) + (k + 2) * 2.0 ** -24) * size)
+    # and the layer is near the one without 8 bits: half a step of 2^-4 in both operands, random signs
+    full = h["x"] @ h["w"].T + h["b"]
+    assert np.linalg.norm(y.cpu().double().numpy() - full) <= 2 * 2.0 ** -4 * np.linalg.norm(full)
+
+
+def test_same_bits_every_time_on_another_stream_and_in_a_graph(hs):
+    rng = np.random.default_rng(31)
+    m, n, k = 300, 260, 2000
+    a, sa, b, sb = dev(*operand(rng, m, k, 2), *operand(rng, n, k, 2))
+    x = torch.from_numpy(rng.standard_normal((m, k)).astype(np.float32)).cuda()
+    ws = torch.empty(16 << 20, dtype=torch.uint8, device="cuda")
+    q, s = buffers(m, k)
+    c, first = torch.empty(m, n, device="cuda"), None
+
+    def work(stream=None):
+        hs.hs_op_quantize_fp8(0, x, k, m, k, 0, q, q.shape[1], s, s.shape[1], stream=stream)
+        hs.hs_op_gemm_fp8(m, n, k, q, q.shape[1], s, s.shape[1], b, b.shape[1], sb, sb.shape[1], c, n, c_f32=1, scratch=ws, scratch_bytes=ws.numel(), stream=stream)
+
+    work()
+    torch.cuda.synchronize()
+    first = c.clone()
+    side = torch.cuda.Stream()
+    c.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    work(side)
+    side.synchronize()
+    assert torch.equal(c, first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for i in range(4):
+        x.mul_(2.0)
+        c.zero_()
+        ws.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c, first * 2.0 ** (i + 1))      # powers of two go through the scales
+
+
+def test_refusals_leave_the_output_alone(hs):
+    c = torch.full((4, 4), 3.0, device="cuda")
+    q = torch.zeros(4, 128, dtype=torch.uint8, device="cuda")
+    s = torch.zeros(4, 4, dtype=torch.uint8, device="cuda")
+    with pytest.raises(hs.HsError):
+        hs.hs_op_gemm_fp8(4, 4, 129, q, 128, s, 4, q, 128, s, 4, c, 4, c_f32=1)
+    with pytest.raises(hs.HsError):
+        hs.hs_op_quantize_fp8(0, c, 4, 4, 4, 0, q, 100, s, 4)
+    torch.cuda.synchronize()
+    assert torch.all(c == 3.0) and torch.all(q == 0)

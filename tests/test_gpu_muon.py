@@ -1,0 +1,355 @@
+"""Orthogonalised matrices and the update made of them on a GPU against the 64-bit oracle."""
+import numpy as np
+import pytest
+
+from oracle import matrix_ops as M
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hs():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2009_14783_amd import binding
+    binding.lib()            # a missing library is a failure, not a skip
+    return binding
+
+
+def rel(a, b):
+    nb = np.linalg.norm(b)
+    return np.linalg.norm(a - b) / nb if nb > 0 else np.linalg.norm(a - b)
+
+
+def tolerance(x, products, **kw):
+    """What the kernels' roundings come to, by the oracle with the same ones: X kept as two numbers of 11 bits, operands of one (16-bit products) or two, 32-bit
+    sums.  (The sums have to be in it: 513 in 32-bit products are 97 additions of up to 2^-24 of the running sum each, which together are more than the
+    2^-23 of a number kept in 22 bits.)  Twice that, for sums in another order; at least 8 of 22 bits.  Roundings that fall otherwise: the
+    error is that of k = min(rows, cols) directions, each of which its own amplification makes a sum of few, so both norms are samples of a
+    distribution with k degrees of freedom, three of whose standard deviations are 3 / sqrt(2 k) of it; 3 / sqrt(k) for the two."""
+    e = M.orthogonalize(x, **kw)
+    return max(2.0 * (1.0 + 3.0 / np.sqrt(min(x.shape))) * rel(M.orthogonalize(x, numbers=1 if products == 1 else 2, **kw), e), 8 * 2.0 ** -22), e
+
+
+def layout(shapes, gap=0, ld=0):
+    """(offset, ld, rows, cols) of matrices one behind the other, and the size of the buffer."""
+    mats, at = [], gap
+    for r, c in shapes:
+        mats.append((at, c + ld, r, c))
+        at += r * (c + ld) + gap
+    return mats, at
+
+
+def view(flat, mat):
+    off, ld, r, c = mat
+    return np.lib.stride_tricks.as_strided(flat[off:], (r, c), (ld * flat.itemsize, flat.itemsize))
+
+
+def workspace(hs, mats, products):
+    n = hs.hs_orthogonalize_workspace_bytes(mats, products)
+    return torch.full((n,), 0x7c, dtype=torch.uint8, device="cuda"), n      # not zeros: nothing may be taken for granted
+
+
+def gaussian(rng, size):
+    return rng.standard_normal(size).astype(np.float32)
+
+
+SHAPES = [(1, 1), (1, 7), (5, 1), (37, 53), (64, 64), (65, 64), (64, 65), (130, 67), (128, 512), (512, 128), (200, 129), (300, 257), (513, 320), (37, 53), (300, 1100)]
+
+
+@pytest.mark.parametrize("products", [0, 1])
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("gap,ld", [(0, 0), (3, 0), (8, 5)])
+def test_list_of_odd_shapes(hs, products, dtype, gap, ld):
+    mats, size = layout(SHAPES, gap, ld)
+    x = torch.from_numpy(gaussian(np.random.default_rng(gap + ld), size)).to(torch.bfloat16 if dtype else torch.float32)
+    y = torch.full_like(x, 7.5).cuda()
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, products)
+    hs.hs_op_orthogonalize(dtype, x.cuda(), y, size, lst, products, 5, None, 1e-7, ws, n)
+    torch.cuda.synchronize()
+    got, flat = y.cpu().double().numpy(), x.double().numpy()
+    for mat in mats:
+        tol, e = tolerance(view(flat, mat), products)
+        assert rel(view(got, mat), e) <= tol + (2.0 ** -8 if dtype else 0.0), mat
+    rest = np.ones(size, bool)
+    for mat in mats:
+        view(rest, mat)[...] = False
+    assert np.all(got[rest] == 7.5)
+
+
+@pytest.mark.parametrize("products", [0, 1])
+@pytest.mark.parametrize("shape,count", [((768, 768), 2), ((1024, 640), 3), ((600, 2000), 2), ((256, 256), 40)])
+def test_larger_matrices(hs, products, shape, count):
+    mats, size = layout([shape] * count)
+    x = gaussian(np.random.default_rng(shape[0]), size)
+    y = torch.empty(size, device="cuda")
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, products)
+    hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, size, lst, products, 5, None, 1e-7, ws, n)
+    got = y.cpu().double().numpy()
+    for mat in mats[:2] + mats[-1:]:
+        tol, e = tolerance(view(x.astype(np.float64), mat), products)
+        assert rel(view(got, mat), e) <= tol
+
+
+@pytest.mark.parametrize("products", [0, 1])
+def test_matrix_of_low_rank_with_noise(hs, products):
+    """Small singular values, which the polynomial multiplies by hundreds: the roundings of the large ones must not go with them."""
+    rng = np.random.default_rng(2)
+    x = (rng.standard_normal((320, 16)) @ rng.standard_normal((16, 400)) + 0.02 * rng.standard_normal((320, 400))).astype(np.float32)
+    lst = hs.make_matrices([(0, 400, 320, 400)])
+    ws, n = workspace(hs, lst, products)
+    y = torch.empty(320, 400, device="cuda")
+    hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, x.size, lst, products, 5, None, 1e-7, ws, n)
+    tol, e = tolerance(x.astype(np.float64), products)
+    assert tol < (3e-3 if products else 5e-5)
+    assert rel(y.cpu().double().numpy(), e) <= tol
+
+
+@pytest.mark.parametrize("products", [0, 1])
+@pytest.mark.parametrize("steps,coeff", [(1, None), (2, [(2.0, -1.5, 0.5), (1.5, -0.5, 0.0)]), (8, None), (12, [(1.875, -1.25, 0.375)] * 12)])
+def test_other_steps_and_coefficients(hs, products, steps, coeff):
+    x = gaussian(np.random.default_rng(steps), 90 * 150)
+    lst = hs.make_matrices([(0, 150, 90, 150)])
+    ws, n = workspace(hs, lst, products)
+    y = torch.empty(x.size, device="cuda")
+    hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, x.size, lst, products, steps, coeff, 1e-7, ws, n)
+    tol, e = tolerance(x.astype(np.float64).reshape(90, 150), products, steps=steps, coeff=coeff)
+    assert rel(y.cpu().double().numpy().reshape(90, 150), e) <= tol
+
+
+@pytest.mark.parametrize("products", [0, 1])
+@pytest.mark.parametrize("factor", [1e-30, 1e-12, 1e30])
+def test_sizes_whose_squares_leave_32_bits(hs, products, factor):
+    x = (gaussian(np.random.default_rng(1), 70 * 80) * np.float32(factor)).astype(np.float32)
+    lst = hs.make_matrices([(0, 80, 70, 80)])
+    ws, n = workspace(hs, lst, products)
+    y = torch.empty(x.size, device="cuda")
+    hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, x.size, lst, products, 5, None, 0.0, ws, n)
+    tol, e = tolerance(x.astype(np.float64).reshape(70, 80), products, eps=0.0)
+    assert rel(y.cpu().double().numpy().reshape(70, 80), e) <= tol
+
+
+def test_zeros_stay_zeros_and_what_is_not_finite_stays_in_its_matrix(hs):
+    mats, size = layout([(40, 50), (40, 50), (40, 50), (50, 40), (3, 3)])
+    x = gaussian(np.random.default_rng(3), size)
+    view(x, mats[0])[...] = 0
+    view(x, mats[1])[3, 4] = np.nan
+    view(x, mats[3])[7, 7] = np.inf
+    lst = hs.make_matrices(mats)
+    for products in (0, 1):
+        for eps in (0.0, 1e-7):
+            ws, n = workspace(hs, lst, products)
+            y = torch.empty(size, device="cuda")
+            hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, size, lst, products, 5, None, eps, ws, n)
+            got = y.cpu().double().numpy()
+            assert np.all(view(got, mats[0]) == 0)
+            assert np.all(np.isnan(view(got, mats[1]))) and np.all(np.isnan(view(got, mats[3])))
+            for mat in (mats[2], mats[4]):
+                tol, e = tolerance(view(x.astype(np.float64), mat), products, eps=eps)
+                assert rel(view(got, mat), e) <= tol
+
+
+def test_many_matrices_and_more_shapes_than_one_launch_takes(hs):
+    """450 matrices of 45 shapes, in an order that mixes them."""
+    rng = np.random.default_rng(5)
+    shapes = [(1 + i % 9, 2 + (i * 7) % 45) for i in range(450)]
+    mats, size = layout(shapes, 1)
+    x = gaussian(rng, size)
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, 0)
+    y = torch.empty(size, device="cuda")
+    hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, size, lst, 0, 5, None, 1e-7, ws, n)
+    got = y.cpu().double().numpy()
+    for mat in mats:
+        tol, e = tolerance(view(x.astype(np.float64), mat), 0)
+        assert rel(view(got, mat), e) <= tol, mat
+
+
+def test_in_place_and_the_same_bits_every_time(hs):
+    mats, size = layout([(100, 300), (300, 100)])
+    x = torch.from_numpy(gaussian(np.random.default_rng(6), size)).cuda()
+    lst = hs.make_matrices(mats)
+    outs = []
+    for place in (False, True, True):
+        ws, n = workspace(hs, lst, 1)
+        src = x.clone()
+        dst = src if place else torch.empty_like(src)
+        hs.hs_op_orthogonalize(0, src, dst, size, lst, 1, 5, None, 1e-7, ws, n)
+        outs.append(dst.clone())
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[1], outs[2])
+
+
+def muon_tolerances(w, m, G, lr, momentum, nesterov, weight_decay, rms, denom, products, **ortho):
+    """(w, its tolerance, m, its tolerance), element by element but for the orthogonalised part, which is off by a share of its norm."""
+    g = G / denom if denom > 0 else G
+    nw, nm, O = M.muon_step(w, m, G, lr, momentum, nesterov, weight_decay, rms, denom, **ortho)
+    u = g + momentum * nm if nesterov else nm
+    tol, e = tolerance(u, products, **ortho)
+    s = rms * np.sqrt(max(w.shape)) if rms > 0 else np.sqrt(max(1.0, w.shape[0] / w.shape[1]))
+    # u itself is 32 bits: a few roundings of 2^-24, which are not amplified more than those of 22 bits
+    wt = 4 * 2.0 ** -24 * (np.linalg.norm(w) + np.linalg.norm(nw)) + abs(lr) * s * (2 * tol) * np.linalg.norm(O)
+    return nw, wt, nm, 4 * 2.0 ** -24 * (np.abs(momentum * m) + np.abs(g))
+
+
+@pytest.mark.parametrize("products", [0, 1])
+@pytest.mark.parametrize("nesterov,denom,rms,wd,lowp", [(1, 48.0, 0.2, 0.1, True), (0, 0.0, 0.0, 0.0, False), (1, 0.0, 0.2, 0.0, True)])
+@pytest.mark.parametrize("gap,ld", [(0, 0), (5, 3)])
+def test_update_of_a_list(hs, products, nesterov, denom, rms, wd, lowp, gap, ld):
+    mats, size = layout([(1, 1), (64, 192), (192, 64), (37, 53), (300, 520), (130, 67)], gap, ld)
+    rng = np.random.default_rng(gap + int(denom))
+    w, m, G = 0.02 * gaussian(rng, size), 1e-3 * gaussian(rng, size), np.float32(max(denom, 1.0)) * 1e-3 * gaussian(rng, size)
+    dw, dm, dG = (torch.from_numpy(a.copy()).cuda() for a in (w, m, G))
+    low = torch.full((size,), 7.5, dtype=torch.bfloat16, device="cuda") if lowp else None
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, products)
+    hs.hs_muon_step(dw, dm, dG, low, size, lst, products, denom, 0.02, 0.95, nesterov, wd, rms, 5, None, 1e-7, ws, n)
+    torch.cuda.synchronize()
+    gw, gm = dw.cpu().double().numpy(), dm.cpu().double().numpy()
+    f = lambda a, mat: view(a.astype(np.float64), mat)
+    for mat in mats:
+        nw, wt, nm, mt = muon_tolerances(f(w, mat), f(m, mat), f(G, mat), 0.02, 0.95, nesterov, wd, rms, denom, products)
+        assert np.linalg.norm(view(gw, mat) - nw) <= wt, mat
+        assert np.all(np.abs(view(gm, mat) - nm) <= mt), mat
+    rest = np.ones(size, bool)
+    for mat in mats:
+        view(rest, mat)[...] = False
+    assert np.array_equal(gw[rest], w[rest].astype(np.float64)) and np.array_equal(gm[rest], m[rest].astype(np.float64))
+    assert torch.equal(dG.cpu(), torch.from_numpy(G))
+    if lowp:
+        want = torch.where(torch.from_numpy(rest), torch.full((size,), 7.5, dtype=torch.bfloat16), dw.cpu().to(torch.bfloat16))
+        assert torch.equal(low.cpu(), want)
+
+
+def test_update_on_another_stream_and_in_a_graph(hs):
+    """Each replay is the next update; eager updates of the same state and other work run between the replays."""
+    mats, size = layout([(128, 384), (384, 128), (100, 100)])
+    rng = np.random.default_rng(9)
+    w0, m0, G0 = 0.02 * gaussian(rng, size), 1e-3 * gaussian(rng, size), 1e-3 * gaussian(rng, size)
+    lst = hs.make_matrices(mats)
+
+    def state():
+        w, m, G = (torch.from_numpy(a.copy()).cuda() for a in (w0, m0, G0))
+        return w, m, G, torch.zeros(size, dtype=torch.bfloat16, device="cuda"), workspace(hs, lst, 1)
+
+    def step(s, stream=None):
+        w, m, G, low, (ws, n) = s
+        hs.hs_muon_step(w, m, G, low, size, lst, 1, 2.0, 1e-3, 0.9, 1, 0.01, 0.2, 5, None, 1e-7, ws, n, stream=stream)
+
+    a, b, c = state(), state(), state()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(b)
+    for k in range(4):
+        step(a)
+        graph.replay()
+        step(c, side)
+        torch.cuda.synchronize()
+        b[4][0].fill_(k)
+        for t in range(4):
+            assert torch.equal(a[t], b[t]) and torch.equal(a[t], c[t])
+        a[2].mul_(0.5), b[2].mul_(0.5), c[2].mul_(0.5)
+        torch.cuda.synchronize()
+
+
+def test_refusal_leaves_the_state_alone(hs):
+    w = torch.ones(100, device="cuda")
+    lst = hs.make_matrices([(0, 10, 10, 10)])
+    with pytest.raises(hs.HsError) as e:
+        hs.hs_muon_step(w, w, w, None, 100, lst, 1, 0.0, 0.1, 0.9, 1, 0.0, 0.2, 5, None, 1e-7, torch.empty(256, dtype=torch.uint8, device="cuda"), 256)
+    assert e.value.status == 3
+    torch.cuda.synchronize()
+    assert torch.all(w == 1)
+
+
+# ---- in the training steps --------------------------------------------------------------------------
+MUON = dict(momentum=0.9, weight_decay=0.01, rms=0.2)
+
+
+def reference_update(layout_, hidden, w, m, v, G, D, adam, t, products, lr=None):
+    """All parameters after one update in 64 bits, and the tolerance of each matrix' part (norm), by (offset, rows, cols)."""
+    w, m, v = w.copy(), m.copy(), v.copy()
+    lr = adam["lr"] if lr is None else lr
+    blocks, rest = [], np.ones(w.size, bool)
+    for name, off, r, c in layout_:
+        if not name.endswith(".w"):
+            continue
+        n = r // hidden if "qkv" in name or "ckv" in name else 1
+        for i in range(n):
+            at = slice(off + i * (r // n) * c, off + (i + 1) * (r // n) * c)
+            nw, wt, nm, mt = muon_tolerances(w[at].reshape(r // n, c), m[at].reshape(r // n, c), G[at].reshape(r // n, c), lr, MUON["momentum"], True,
+                                             MUON["weight_decay"], MUON["rms"], D, products)
+            w[at], m[at] = nw.reshape(-1), nm.reshape(-1)
+            blocks.append((at, wt))
+            rest[at] = False
+    g = G[rest] / D
+    m[rest] = adam["beta1"] * m[rest] + (1 - adam["beta1"]) * g
+    v[rest] = adam["beta2"] * v[rest] + (1 - adam["beta2"]) * g * g
+    w[rest] -= adam["lr"] * (m[rest] / (1 - adam["beta1"] ** t)) / (np.sqrt(v[rest] / (1 - adam["beta2"] ** t)) + adam["eps"])
+    return w, m, v, blocks, rest
+
+
+@pytest.mark.parametrize("compute", ["fp32", "bf16"])
+@pytest.mark.parametrize("which", ["encoder", "pairs"])
+def test_training_steps_with_matrix_updates(hs, compute, which):
+    from paper_2009_14783_amd import synth
+    from paper_2009_14783_amd.step import PairWorker, Worker
+    pairs = which == "pairs"
+    model = synth.S2S_MODELS["s2s_tiny"] if pairs else synth.MODELS["tiny"]
+    lay = hs.hs_s2s_param_layout(hs.make_s2s_cfg(**model)) if pairs else hs.hs_param_layout(hs.make_cfg(**model))
+    theta = synth.init_params(lay, 11)
+    worker = (PairWorker if pairs else Worker)(model, compute, theta)
+    rng = synth.rng_for(12)
+    mbs = [synth.make_pair_batch(rng, [16, 9, 24], [20, 32, 7], 24, 32, model["vocab"], "uniform") if pairs else
+           synth.make_micro_batch(rng, [16, 32, 48, 64], 64, model["vocab"], "uniform") for _ in range(2)]
+    batches = [worker.upload(mb) for mb in mbs]
+    adam = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-6)
+    products = 1 if compute == "bf16" else 0
+    h = lambda t: t.cpu().double().numpy()
+    for t in (1, 2, 3):
+        before = [h(x) for x in (worker.w, worker.m, worker.v)]
+        D = worker.train_step(batches, adam, muon=MUON if t < 3 else dict(MUON, lr=5e-3))
+        torch.cuda.synchronize()
+        assert worker.t == t
+        G = h(worker.G)
+        lr = None if t < 3 else 5e-3
+        # the matrices' share of G holds the sums, Adam's share was divided in place
+        mats = np.zeros(G.size, bool)
+        for name, off, r, c in lay:
+            if name.endswith(".w"):
+                mats[off:off + r * c] = True
+        sums = np.where(mats, G, G * D)
+        w, m, v, blocks, rest = reference_update(lay, model["hidden"], *before, sums, float(D), adam, t, products, lr)
+        gw = h(worker.w)
+        for at, wt in blocks:
+            assert np.linalg.norm(gw[at] - w[at]) <= wt
+        assert rel(h(worker.m), m) <= 8 * 2.0 ** -24 and rel(h(worker.v)[rest], v[rest]) <= 16 * 2.0 ** -24
+        assert np.all(h(worker.v)[~rest] == 0)
+        # Adam's quotient: a few roundings of its own value
+        assert np.all(np.abs(gw[rest] - w[rest]) <= 8 * 2.0 ** -24 * np.abs(w[rest]) + 64 * 2.0 ** -24 * adam["lr"] * 40)
+        if worker.w_lowp is not None:
+            assert torch.equal(worker.w_lowp, worker.w.to(torch.bfloat16))
+    assert np.isfinite(np.sum(worker.reported_loss(D)))
+    worker.close()
+
+
+def test_step_without_data_and_loop(hs):
+    """A worker without data moves its weights by the momentum alone; the loop hands the schedule's rate on."""
+    from paper_2009_14783_amd import synth
+    from paper_2009_14783_amd.step import Worker
+    model = synth.MODELS["tiny"]
+    lay = hs.hs_param_layout(hs.make_cfg(**model))
+    worker = Worker(model, "fp32", synth.init_params(lay, 1))
+    adam = dict(beta1=0.9, beta2=0.999, eps=1e-6)
+    losses = worker.train(3, lambda t: synth.step_micro_batches(5, t, [16, 32], 32, model["vocab"], "uniform"), adam, dict(max_lr=1e-3, warmup=2, total=10), muon=MUON)
+    assert len(losses) == 3 and np.all(np.isfinite(losses)) and worker.t == 3
+    m = worker.m.clone()
+    worker.train_step([None], dict(adam, lr=1e-3), denom=4, muon=MUON)
+    torch.cuda.synchronize()
+    off, r, c = next((o, r, c) for name, o, r, c in lay if name == "l0.o.w")
+    assert torch.allclose(worker.m[off:off + r * c], 0.9 * m[off:off + r * c], rtol=2.0 ** -23, atol=0)
+    worker.close()
