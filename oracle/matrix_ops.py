@@ -89,10 +89,11 @@ def _sum32(pairs):
     return c
 
 
-def orthogonalize(x, steps=5, coeff=None, eps=1e-7, numbers=None):
+def orthogonalize(x, steps=5, coeff=None, eps=1e-7, numbers=None, runs=None):
     """O(x).  numbers: None for 64-bit arithmetic throughout; 1 or 2 for products of operands rounded to that many numbers of 11 bits each (two: hi hi + hi lo +
     lo hi), summed in 32 bits, where X is always kept as two such numbers and everything between the products is 32 bits: how the roundings of products
-    in fewer bits are derived."""
+    in fewer bits are derived.  runs: with numbers, the steps are taken in runs of these lengths, each on A alone (S_i from A_i, A_(i+1) = S_i A_i S_i, the product Q
+    of the run's S_i applied to X at its end), every one of these matrices rounded off its diagonal."""
     f32 = (lambda p: p) if numbers is None else (lambda p: np.asarray(p, dtype=np.float32).astype(np.float64))
 
     def parts(p):
@@ -111,6 +112,31 @@ def orthogonalize(x, steps=5, coeff=None, eps=1e-7, numbers=None):
     X = f32(x / (norm + eps)) if norm != 0 else np.zeros_like(x)
     tall = X.shape[0] > X.shape[1]
     X = X.T if tall else X
+    if numbers is not None and runs is not None:
+        def kept(p):
+            d = np.diag(np.diag(p))
+            return f32(d) + sum(parts(p - d)[:numbers])
+
+        def both(p, q):
+            """Product of two kept matrices: the parts off the diagonal by times(), the rest in 32 bits."""
+            dp, dq = np.diag(p), np.diag(q)
+            e, f = p - np.diag(dp), q - np.diag(dq)
+            return f32(f32(times(e, f) + f32(dp[:, None] * f)) + f32(e * dq[None, :])) + np.diag(f32(dp * dq))
+
+        k = 0
+        for n in runs:
+            X = f32(sum(parts(X)))
+            A, Q = kept(times(X, X.T)), None
+            for j in range(n):
+                a, b, c = coeff[k + j]
+                S = kept(f32(f32(a * np.eye(len(A)) + b * A) + f32(c * both(A, A))))
+                if j + 1 < n:
+                    A = kept(both(kept(both(S, A)), S))
+                Q = S if Q is None else kept(both(S, Q))
+            d = np.diag(Q)
+            X = f32(f32(d[:, None] * X) + times(Q - np.diag(d), X))
+            k += n
+        return X.T if tall else X
     for a, b, c in coeff:
         if numbers is None:
             A = X @ X.T

@@ -156,6 +156,55 @@ __device__ __forceinline__ void mma_loop(int nk, unsigned char* lds_raw, f32x16 
   asm volatile("" ::: "memory");
 }
 
+// For products of few tiles, where the chain of latencies through the contraction is what counts: every wave of the block forms the whole 32 x 32 tile over the
+// k-tiles w, w + NW, ..., from a ring of S stages of its own at `ring` and without a barrier; the tiles are added in wave order.  What comes back in acc is the sum,
+// in wave 0.  next(dst) requests the wave's next k-tile (or, once they are used up, something harmless); scales(t): the t-th one is about to be used.
+template <class MMA, class TA, class TB, int NW, int S, class Next, class Scales>
+__device__ __forceinline__ void ks_loop(int nk, unsigned char* lds_raw, f32x16& acc, const int& sa, const int& sb, int lane, int wave, Next&& next,
+                                        Scales&& scales) {
+  constexpr int KS = MMA::KS, STAGE = TA::BYTES + TB::BYTES, NL = TA::NI + TB::NI;
+  unsigned char* const ring = lds_raw + wave * S * STAGE;
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) next(ring + s * STAGE);
+  for (int t0 = 0; t0 < nk; t0 += S) {
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+      const int t = t0 + u;
+      if (t >= nk) break;
+      asm volatile("" ::: "memory");
+      wait_loads<(S - 2) * NL>();
+      asm volatile("" ::: "memory");
+      next(ring + ((u + S - 1) % S) * STAGE);      // its last reads are done: their results went into the last matrix instructions
+      scales(t);
+      const bf16* sA = (const bf16*)(ring + u * STAGE);
+      const bf16* sB = (const bf16*)(ring + u * STAGE + TA::BYTES);
+      typename MMA::Frag fa[KS], fb[KS];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) { fa[k] = MMA::template frag<TA>(sA, 0, k, lane); fb[k] = MMA::template frag<TB>(sB, 0, k, lane); }
+#pragma unroll
+      for (int k = 0; k < KS; ++k) MMA::mma(MMA::op(fa[k], sa), MMA::op(fb[k], sb), acc, sa, sb);
+    }
+  }
+  asm volatile("" ::: "memory");
+  wait_loads<0>();
+  __syncthreads();               // the rings become the waves' tiles
+  float4* const red = (float4*)lds_raw;
+  if (wave > 0) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) red[((wave - 1) * 4 + q) * 64 + lane] = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+  }
+  __syncthreads();
+  if (wave == 0) {
+#pragma unroll
+    for (int w = 0; w < NW - 1; ++w)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 v = red[(w * 4 + q) * 64 + lane];
+        acc[4 * q] += v.x; acc[4 * q + 1] += v.y; acc[4 * q + 2] += v.z; acc[4 * q + 3] += v.w;
+      }
+  }
+}
+
 template <int TI, int TJ>
 __device__ __forceinline__ void clear_tiles(f32x16 (&acc)[TI][TJ]) {
 #pragma unroll

@@ -16,48 +16,55 @@
 #include <algorithm>
 #include <cmath>
 #include <numeric>
+#include <tuple>
 
 #include "mma_tile.h"
 
 namespace {
 
-constexpr int kGroups = 16;           // shapes of one launch
+constexpr int kJobs = 16;             // jobs of one launch
 constexpr int kParts = 256;           // partial sums of a matrix' norm, at most
-constexpr int kPartElems = 16384;     // ... of so many elements at least
-constexpr float kSx = 256.0f, kSa = 4096.0f, kSs = 1024.0f;
+constexpr int kPartElems = 4096;      // ... of so many elements at least (but the last)
+constexpr float kSx = 256.0f;         // X is held times this
+
+// The square matrices that a matrix has beside its X, each in fp16 with its diagonal apart in 32 bits, times the factor of its kind.
+enum { BUF_A = 0, BUF_S, BUF_T, BUF_Q, BUF_Q2, BUFS };
+__host__ __device__ constexpr float buf_scale(int b) { return b == BUF_A || b == BUF_T ? 4096.0f : b == BUF_S ? 1024.0f : 64.0f; }
 
 // Matrices of one shape; `first` is the place of the first one in the table of offsets.
 struct NsGroup {
-  int rows, cols, m, n, tall, count, first, parts;
+  int rows, cols, m, n, tall, count, first, parts, bufs;
   int64_t ws, stride;      // bytes: first matrix' part of the workspace, and from one matrix to the next
 };
+// What a launch does to the matrices of a group.  Symmetric products: out = ident I + alpha P + beta P Q.
+struct NsJob { NsGroup g; int p, q, out; float ident, alpha, beta; };
 struct NsPlace { int64_t offset, ld; };      // a matrix in the flat buffers
 struct NsDev {
-  int ng, split;           // split: 32-bit products
-  int first_block[kGroups + 1];
-  NsGroup g[kGroups];
+  int n, split;            // jobs; split: 32-bit products
+  int first_block[kJobs + 1];
+  NsJob job[kJobs];
   char* ws;
   const NsPlace* table;
   double* partial;         // [matrices][kParts]
   int from;                // which of the two X is read
-  float a, b, c;
 };
-static_assert(sizeof(NsDev) < 2048, "kernel arguments");
+static_assert(sizeof(NsDev) < 3072, "kernel arguments");
 
-// parts of a matrix' workspace
-struct NsParts { size_t x, a, s, diag, total; };      // x: bytes of one X (both its numbers); the other one is behind it
-__host__ __device__ inline NsParts ns_parts(int m, int n, int split) {
-  NsParts p;
-  const size_t x = (size_t)m * n * 2, a = (size_t)m * m * 2;
-  p.x = 2 * x; p.a = 4 * x; p.s = p.a + (split ? 2 : 1) * a; p.diag = p.s + (split ? 2 : 1) * a;
-  p.total = (p.diag + (size_t)m * 4 + 255) & ~(size_t)255;
-  return p;
+// parts of a matrix' workspace: two X of two numbers each, the square matrices (of two numbers each for 32-bit products), their diagonals
+__host__ __device__ inline size_t x_bytes(const NsGroup& g) { return (size_t)g.m * g.n * 4; }
+__host__ __device__ inline size_t buf_bytes(const NsGroup& g, int split) { return (size_t)g.m * g.m * (split ? 4 : 2); }
+__device__ __forceinline__ f16* buf_ptr(char* base, const NsGroup& g, int split, int b) { return (f16*)(base + 2 * x_bytes(g) + b * buf_bytes(g, split)); }
+__device__ __forceinline__ float* diag_ptr(char* base, const NsGroup& g, int split, int b) {
+  return (float*)(base + 2 * x_bytes(g) + g.bufs * buf_bytes(g, split)) + (int64_t)b * g.m;
+}
+size_t matrix_bytes(const NsGroup& g, int split) {
+  return align_up(2 * x_bytes(g) + g.bufs * (buf_bytes(g, split) + (size_t)g.m * sizeof(float)), 256);
 }
 
-// the group, matrix and block within the matrix of this thread block, whose matrices have `per` blocks each
-__device__ __forceinline__ int ns_group(const NsDev& d, int v) {
+// the job that thread block v works on
+__device__ __forceinline__ int ns_job(const NsDev& d, int v) {
   int i = 0;
-  while (i + 1 < d.ng && v >= d.first_block[i + 1]) ++i;
+  while (i + 1 < d.n && v >= d.first_block[i + 1]) ++i;
   return i;
 }
 
@@ -76,32 +83,64 @@ struct MuonIO {
 };
 struct PlainIO { const void* x; void* y; int bf; };
 
-__device__ __forceinline__ float plain_at(const PlainIO& io, int64_t i) { return io.bf ? (float)((const bf16*)io.x)[i] : ((const float*)io.x)[i]; }
+// Four neighbours of a row from element i on, `have` of which exist (whole: all, and i is a multiple of 4).
+__device__ __forceinline__ float4 load4(const float* __restrict__ p, int64_t i, int have, bool whole) {
+  if (whole) return *(const float4*)(p + i);
+  return make_float4(have > 0 ? p[i] : 0.0f, have > 1 ? p[i + 1] : 0.0f, have > 2 ? p[i + 2] : 0.0f, have > 3 ? p[i + 3] : 0.0f);
+}
+__device__ __forceinline__ float4 gradient4(const MuonIO& io, int64_t i, int have, bool whole) {
+  float4 g = load4(io.G, i, have, whole);
+  if (io.denom > 0.0f) { g.x /= io.denom; g.y /= io.denom; g.z /= io.denom; g.w /= io.denom; }
+  return g;
+}
+__device__ __forceinline__ float4 plain4(const PlainIO& io, int64_t i, int have, bool whole) {
+  if (!io.bf) return load4((const float*)io.x, i, have, whole);
+  const bf16* const p = (const bf16*)io.x;
+  if (whole) {
+    const bf16x4 v = *(const bf16x4*)(p + i);
+    return make_float4((float)v[0], (float)v[1], (float)v[2], (float)v[3]);
+  }
+  return make_float4(have > 0 ? (float)p[i] : 0.0f, have > 1 ? (float)p[i + 1] : 0.0f, have > 2 ? (float)p[i + 2] : 0.0f, have > 3 ? (float)p[i + 3] : 0.0f);
+}
+__device__ __forceinline__ float axpy1(const MuonIO& io, float m, float g) { return io.nesterov ? g + io.mu * m : m; }
 
 // First pass: the momentum is updated, and the sum of squares of what is going to be orthogonalised is formed in 64 bits (gradients of 1e-25 have squares
 // that 32 bits do not hold), a part of a matrix per block, added in a fixed order.  Memory bound: 12 bytes per element.
 template <class IO>
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsDev d, IO io) {
-  const int gi = ns_group(d, blockIdx.x);
-  const NsGroup& g = d.g[gi];
-  const int local = blockIdx.x - d.first_block[gi], mat = local / g.parts, part = local % g.parts;
+  const int ji = ns_job(d, blockIdx.x);
+  const NsGroup& g = d.job[ji].g;
+  const int local = blockIdx.x - d.first_block[ji], mat = local / g.parts, part = local % g.parts;
   const NsPlace at = d.table[g.first + mat];
-  const int64_t total = (int64_t)g.rows * g.cols, chunk = (total + g.parts - 1) / g.parts;
-  const int64_t end = min(total, (part + 1) * chunk);
+  // a matrix without gaps is one long row
+  const bool flat = at.ld == g.cols;
+  const int cols = flat ? g.rows * g.cols : g.cols, per_row = (cols + 3) / 4, total = (flat ? 1 : g.rows) * per_row;
+  const int chunk = (total + g.parts - 1) / g.parts, end = min(total, (part + 1) * chunk);
+  const bool quads = ((at.offset | (flat ? 0 : at.ld)) & 3) == 0;
   double sum = 0.0;
-  for (int64_t e = part * chunk + threadIdx.x; e < end; e += 256) {
-    const int64_t r = e / g.cols, i = at.offset + r * at.ld + (e - r * g.cols);
-    float u;
+#pragma unroll 4
+  for (int e = part * chunk + threadIdx.x; e < end; e += 256) {
+    const int r = flat ? 0 : e / per_row, c = (e - r * per_row) * 4, have = cols - c;
+    const int64_t i = at.offset + r * at.ld + c;
+    const bool whole = quads && have >= 4;
+    float4 u;
     if constexpr (std::is_same<IO, MuonIO>::value) {
-      float gr = io.G[i];
-      if (io.denom > 0.0f) gr /= io.denom;
-      const float m = io.mu * io.m[i] + gr;
-      io.m[i] = m;
-      u = io.nesterov ? gr + io.mu * m : m;
+      const float4 gr = gradient4(io, i, have, whole);
+      float4 m = load4(io.m, i, have, whole);
+      m.x = io.mu * m.x + gr.x; m.y = io.mu * m.y + gr.y; m.z = io.mu * m.z + gr.z; m.w = io.mu * m.w + gr.w;
+      if (whole) {
+        *(float4*)(io.m + i) = m;
+      } else {
+        io.m[i] = m.x;
+        if (have > 1) io.m[i + 1] = m.y;
+        if (have > 2) io.m[i + 2] = m.z;
+        if (have > 3) io.m[i + 3] = m.w;
+      }
+      u = make_float4(axpy1(io, m.x, gr.x), axpy1(io, m.y, gr.y), axpy1(io, m.z, gr.z), axpy1(io, m.w, gr.w));
     } else {
-      u = plain_at(io, i);
+      u = plain4(io, i, have, whole);
     }
-    sum += (double)u * (double)u;
+    sum += ((double)u.x * (double)u.x + (double)u.y * (double)u.y) + ((double)u.z * (double)u.z + (double)u.w * (double)u.w);
   }
   __shared__ double red[4];
 #pragma unroll
@@ -111,16 +150,36 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsDev d, IO io) {
   if (threadIdx.x == 0) d.partial[(int64_t)(g.first + mat) * kParts + part] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Second pass: X = U / (|U| + eps) in two fp16 numbers, the shorter side as rows, zeros in the padding.  64 x 64 elements per block.
+// Second pass: X = U / (|U| + eps) in two fp16 numbers, the shorter side as rows, zeros in the padding.  64 x 64 elements per block, turned in LDS if the
+// matrix is tall.  Memory bound: 12 bytes per element.
 template <class IO>
 __global__ __launch_bounds__(256) void ns_start_kernel(NsDev d, IO io, double eps) {
-  const int gi = ns_group(d, blockIdx.x);
-  const NsGroup& g = d.g[gi];
-  const int nbn = g.n / 64, per = g.m / 64 * nbn, local = blockIdx.x - d.first_block[gi], mat = local / per, t = local % per;
+  const int ji = ns_job(d, blockIdx.x);
+  const NsGroup& g = d.job[ji].g;
+  const int nbn = g.n / 64, per = g.m / 64 * nbn, local = blockIdx.x - d.first_block[ji], mat = local / per, t = local % per;
   const int i0 = t / nbn * 64, j0 = t % nbn * 64;
   const NsPlace at = d.table[g.first + mat];
   __shared__ float tile[64][65];
   __shared__ double inv_s;
+  const bool quads = ((at.offset | at.ld) & 3) == 0;
+  const int r0 = g.tall ? j0 : i0, c0 = (g.tall ? i0 : j0) + (threadIdx.x & 15) * 4;
+  float4 u[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = r0 + k * 16 + (threadIdx.x >> 4), have = r < g.rows ? g.cols - c0 : 0;
+    const int64_t i = at.offset + r * at.ld + c0;
+    const bool whole = quads && have >= 4;
+    if constexpr (std::is_same<IO, MuonIO>::value) {
+      const float4 m = load4(io.m, i, have, whole);
+      u[k] = m;
+      if (io.nesterov) {
+        const float4 gr = gradient4(io, i, have, whole);
+        u[k] = make_float4(axpy1(io, m.x, gr.x), axpy1(io, m.y, gr.y), axpy1(io, m.z, gr.z), axpy1(io, m.w, gr.w));
+      }
+    } else {
+      u[k] = plain4(io, i, have, whole);
+    }
+  }
   if (threadIdx.x < 64) {
     double s = 0.0;
     for (int k = threadIdx.x; k < g.parts; k += 64) s += d.partial[(int64_t)(g.first + mat) * kParts + k];
@@ -130,30 +189,22 @@ __global__ __launch_bounds__(256) void ns_start_kernel(NsDev d, IO io, double ep
   }
   __syncthreads();
   const double inv = inv_s;
-  const int r0 = g.tall ? j0 : i0, c0 = g.tall ? i0 : j0;
-  for (int e = threadIdx.x; e < 4096; e += 256) {
-    const int lr = e >> 6, lc = e & 63, r = r0 + lr, c = c0 + lc;
-    float u = 0.0f;
-    if (r < g.rows && c < g.cols) {
-      const int64_t i = at.offset + r * at.ld + c;
-      if constexpr (std::is_same<IO, MuonIO>::value) {
-        u = io.m[i];
-        if (io.nesterov) { float gr = io.G[i]; if (io.denom > 0.0f) gr /= io.denom; u = gr + io.mu * u; }
-      } else {
-        u = plain_at(io, i);
-      }
-      u = (float)((double)u * inv);
-    }
-    if (g.tall) tile[lc][lr] = u; else tile[lr][lc] = u;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int lr = k * 16 + (threadIdx.x >> 4), lc = (threadIdx.x & 15) * 4;
+    const float x[4] = {(float)((double)u[k].x * inv), (float)((double)u[k].y * inv), (float)((double)u[k].z * inv), (float)((double)u[k].w * inv)};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) if (g.tall) tile[lc + c][lr] = x[c]; else tile[lr][lc + c] = x[c];
   }
   __syncthreads();
   f16* const hi = (f16*)(d.ws + g.ws + mat * g.stride);
   f16* const lo = hi + (int64_t)g.m * g.n;
-  for (int e = threadIdx.x; e < 512; e += 256) {
-    const int r = e >> 3, c = (e & 7) * 8;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int e = k * 256 + threadIdx.x, r = e >> 3, c = (e & 7) * 8;
     f16x8 h, l;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) { const float x = tile[r][c + k]; h[k] = (f16)x; l[k] = (f16)(x - (float)h[k]); }
+    for (int q = 0; q < 8; ++q) { const float x = tile[r][c + q]; h[q] = (f16)x; l[q] = (f16)(x - (float)h[q]); }
     const int64_t o = (int64_t)(i0 + r) * g.n + j0 + c;
     *(f16x8*)(hi + o) = h;
     *(f16x8*)(lo + o) = l;
@@ -161,7 +212,7 @@ __global__ __launch_bounds__(256) void ns_start_kernel(NsDev d, IO io, double ep
 }
 
 // ---- the products ---------------------------------------------------------------------------------
-enum { NS_GRAM = 0, NS_SQUARE, NS_APPLY, NS_LAST };
+enum { NS_GRAM = 0, NS_SYM, NS_APPLY, NS_LAST };
 
 // the tile (row, column >= row) of number t of a symmetric matrix of nb x nb tiles
 __device__ __forceinline__ void upper_tile(int t, int nb, int& ti, int& tj) {
@@ -172,192 +223,413 @@ __device__ __forceinline__ void upper_tile(int t, int nb, int& ti, int& tj) {
   ti = r; tj = r + t - (r * nb - r * (r - 1) / 2);
 }
 
-template <class C, int OP, class IO>
-__global__ __launch_bounds__(C::NT) __attribute__((amdgpu_waves_per_eu(C::WPE, C::WPE)))
-void ns_product_kernel(NsDev d, IO io) {
-  constexpr int TI = C::TI, TJ = C::TJ, WN = 32 * TJ, LDW = WN + 4;
-  constexpr bool SYM = OP == NS_GRAM || OP == NS_SQUARE;
-  typedef DmaTile<true, C::BK, C::BM, C::NW> TA;
-  typedef DmaTile<SYM, C::BK, C::BN, C::NW> TB;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / C::WGN, wn = wave % C::WGN;
-  int v = blockIdx.x;      // a contiguous range of tiles per XCD
-  const int per_xcd = (int)gridDim.x >> 3;
-  if (v < 8 * per_xcd) v = (v & 7) * per_xcd + (v >> 3);
-  const int gi = ns_group(d, v);
-  const NsGroup& g = d.g[gi];
-  const int m = g.m, n = g.n, nbm = (m + C::BM - 1) / C::BM, nbn = (n + C::BN - 1) / C::BN;
-  const int per = SYM ? nbm * (nbm + 1) / 2 : nbm * nbn, local = v - d.first_block[gi], mat = local / per, t = local % per;
-  int ti, tj;
-  if (SYM) upper_tile(t, nbm, ti, tj);
-  else tile_of_block<4>(t, nbn, nbm, ti, tj);
-  const int m0 = ti * C::BM, n0 = tj * C::BN;
-  const NsParts parts = ns_parts(m, n, d.split);
-  char* const base = d.ws + g.ws + mat * g.stride;
-  f16* const X = (f16*)(base + d.from * parts.x);
-  f16* const Xn = (f16*)(base + (d.from ^ 1) * parts.x);
-  f16* const A = (f16*)(base + parts.a);
-  f16* const Sm = (f16*)(base + parts.s);
-  float* const diag = (float*)(base + parts.diag);
-
-  // operands, and how far behind the first numbers the second ones are (bytes)
-  const f16* const opA = OP == NS_GRAM ? X : OP == NS_SQUARE ? A : Sm;
-  const f16* const opB = OP == NS_SQUARE ? A : X;
-  const int K = OP == NS_GRAM ? n : m;
-  const int64_t sizeA = (int64_t)m * K * 2, sizeB = OP == NS_SQUARE ? sizeA : (int64_t)m * n * 2;
-  const int nk1 = K / 64, nseg = d.split ? 3 : 1;
-  typename TA::Cursor ca;
-  typename TB::Cursor cb;
-  TA::init(ca, (const bf16*)opA, K, m0, m, 0, K, lane, wave);
-  if (SYM) TB::init(cb, (const bf16*)opB, K, n0, m, 0, K, lane, wave);
-  else TB::init(cb, (const bf16*)opB, n, n0, n, 0, K, lane, wave);
-  ca.rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)opA, 0, (int)(d.split ? 2 * sizeA : sizeA), 0x00020000);
-  cb.rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)opB, 0, (int)(d.split ? 2 * sizeB : sizeB), 0x00020000);
-  int kt = 0, seg = 0;
-  auto next = [&](unsigned char* dst) __attribute__((always_inline)) {
-    if (kt == nk1) {      // hi hi, hi lo, lo hi; then behind the operands
-      kt = 0; ++seg;
-      ca.soff = seg >= nseg ? 0x80000000u : seg == 2 ? (unsigned)sizeA : 0u;
-      cb.soff = seg >= nseg ? 0x80000000u : seg == 1 ? (unsigned)sizeB : 0u;
-    }
-    ++kt;
-    TA::issue(ca, dst, wave);
-    TB::issue(cb, dst + TA::BYTES, wave);
-  };
-  f32x16 acc[TI][TJ];
-  clear_tiles(acc);
-  int sa[TI] = {}, sb[TJ] = {};
-  mma_loop<C, MmaF16, TA, TB>(nk1 * nseg, lds_raw, acc, sa, sb, wm, wn, lane, next, [](int) {});
-
-  const int rbase = m0 + wm * TI * 32, cbase = n0 + wn * TJ * 32;
-  float* const stage = (float*)lds_raw + wave * C::EPI_FLOATS;
-  const NsPlace at = OP == NS_LAST ? d.table[g.first + mat] : NsPlace{0, 0};
-  float step = 0.0f;
-  if constexpr (OP == NS_LAST && std::is_same<IO, MuonIO>::value)
-    step = io.lr * (io.rms > 0.0f ? io.rms * sqrtf((float)max(g.rows, g.cols)) : sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)));
-  // a result that leaves
-  auto emit = [&](int r, int c, float y) __attribute__((always_inline)) {
-    const int64_t i = at.offset + r * at.ld + c;
-    if constexpr (std::is_same<IO, MuonIO>::value) {
-      const float w = io.decay * io.w[i] - step * y;
-      io.w[i] = w;
-      if (io.wl) io.wl[i] = (bf16)w;
-    } else {
-      if (io.bf) ((bf16*)io.y)[i] = (bf16)y; else ((float*)io.y)[i] = y;
-    }
-  };
+__device__ __forceinline__ void to_f8(const f16x8& h, float (&x)[8]) {
 #pragma unroll
-  for (int i = 0; i < TI; ++i) {
-#pragma unroll
-    for (int j = 0; j < TJ; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) stage[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * LDW + j * 32 + (lane & 31)] = acc[i][j][r];
-#pragma unroll
-    for (int it = 0; it < 32 * WN / 8 / 64; ++it) {      // 8 columns of a row per lane
-      const int piece = it * 64 + lane, lr = piece / (WN / 8), lc = (piece % (WN / 8)) * 8;
-      const int row = rbase + i * 32 + lr, col = cbase + lc;
-      if (row >= m || col >= (SYM ? m : n)) continue;
-      float x[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = stage[lr * LDW + lc + k];
-      f16x8 h, l;
-      if (OP == NS_GRAM) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] *= kSa / (kSx * kSx);
-      } else if (OP == NS_SQUARE) {
-        const f16x8 ah = *(const f16x8*)(A + (int64_t)row * m + col);
-        f16x8 al = {};
-        if (d.split) al = *(const f16x8*)(A + (int64_t)m * m + (int64_t)row * m + col);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float s = d.b * (((float)ah[k] + (float)al[k]) * (1.0f / kSa)) + d.c * (x[k] * (1.0f / (kSa * kSa)));
-          if (row == col + k) { diag[row] = s; x[k] = 0.0f; } else x[k] = s * kSs;
-        }
-      } else {
-        const int64_t o = (int64_t)row * n + col;
-        const f16x8 xh = *(const f16x8*)(X + o), xl = *(const f16x8*)(X + (int64_t)m * n + o);
-        const float f = d.a + diag[row];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = f * ((float)xh[k] + (float)xl[k]) + x[k] * (1.0f / kSs);
-      }
-      if (OP == NS_LAST) {
-        if (!g.tall) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) if (row < g.rows && col + k < g.cols) emit(row, col + k, x[k] * (1.0f / kSx));
-        }
-      } else {
-        f16* const out = OP == NS_GRAM ? A : OP == NS_SQUARE ? Sm : Xn;
-        const int ld = SYM ? m : n;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { h[k] = (f16)x[k]; l[k] = (f16)(x[k] - (float)h[k]); }
-        *(f16x8*)(out + (int64_t)row * ld + col) = h;
-        if (!SYM || d.split) *(f16x8*)(out + (int64_t)m * ld + (int64_t)row * ld + col) = l;
-      }
-      if (OP == NS_SQUARE || OP == NS_LAST) {      // what the transposed way out reads
-#pragma unroll
-        for (int k = 0; k < 8; ++k) stage[lr * LDW + lc + k] = x[k];
-      }
-    }
-    if (SYM && ti != tj) {      // the mirror image: 8 rows of a column per lane
-      f16* const out = OP == NS_GRAM ? A : Sm;
-#pragma unroll
-      for (int it = 0; it < 32 * WN / 8 / 64; ++it) {
-        const int piece = it * 64 + lane, lc = piece % WN, lr = piece / WN * 8;
-        const int row = rbase + i * 32 + lr, col = cbase + lc;
-        if (row >= m || col >= m) continue;
-        f16x8 h, l;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float x = stage[(lr + k) * LDW + lc];
-          if (OP == NS_GRAM) x *= kSa / (kSx * kSx);
-          h[k] = (f16)x; l[k] = (f16)(x - (float)h[k]);
-        }
-        *(f16x8*)(out + (int64_t)col * m + row) = h;
-        if (d.split) *(f16x8*)(out + (int64_t)m * m + (int64_t)col * m + row) = l;
-      }
-    }
-    if (OP == NS_LAST && g.tall) {
-#pragma unroll
-      for (int it = 0; it < 32 * WN / 8 / 64; ++it) {
-        const int piece = it * 64 + lane, lc = piece % WN, lr = piece / WN * 8;
-        const int row = rbase + i * 32 + lr, col = cbase + lc;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (row + k < g.cols && col < g.rows) emit(col, row + k, stage[(lr + k) * LDW + lc] * (1.0f / kSx));
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  }
+  for (int k = 0; k < 8; ++k) x[k] = (float)h[k];
 }
 
+// GRAM: A = X X^T.  SYM: products of square matrices that commute (polynomials of A), whose diagonals are kept apart: with P = D + E and Q = D' + E' the
+// matrix instruction forms E E', and D E' + E D' + D D' are added on the way out.  Both are symmetric: tiles on and above the diagonal only, each
+// written in its place and mirrored.  APPLY: X <- (D + E) X, where X is read in 16 bits by the product with E and in full by D X.  LAST: the same on its way out.
+// bytes of LDS of a wave on the way out, and of a block
+template <class C, int OP, bool SPLIT>
+constexpr int ns_wave_bytes() { return C::EPI_FLOATS * 4 + (OP == NS_GRAM || OP == NS_SYM ? (SPLIT ? 2 : 1) * 32 * (32 * C::TJ + 8) * 2 : 0); }
+template <class C, int OP, bool SPLIT>
+constexpr size_t ns_lds() { return std::max(C::KW * C::PIPE, (size_t)C::NS * ns_wave_bytes<C, OP, SPLIT>()); }      // KW > 1: a ring per wave
+
+template <class C, int OP, bool SPLIT, class IO>
+__global__ __launch_bounds__(C::NT) __attribute__((amdgpu_waves_per_eu(C::WPE, C::WPE)))
+void ns_product_kernel(NsDev d, IO io) {
+  constexpr int TI = C::TI, TJ = C::TJ, WN = 32 * TJ, LDW = WN + 4, NIT = 32 * WN / 8 / 64;
+  constexpr bool SYMM = OP == NS_GRAM || OP == NS_SYM;
+  constexpr bool UPDATE = OP == NS_LAST && std::is_same<IO, MuonIO>::value;
+  constexpr bool KSPLIT = C::KW > 1;      // the waves split the contraction (ks_loop)
+  typedef DmaTile<true, C::BK, C::BM, C::NS> TA;
+  typedef DmaTile<SYMM, C::BK, C::BN, C::NS> TB;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = KSPLIT ? 0 : wave / C::WGN, wn = KSPLIT ? 0 : wave % C::WGN, lw = KSPLIT ? 0 : wave;
+  const int ji = ns_job(d, blockIdx.x);
+  const NsJob& job = d.job[ji];
+  const NsGroup& g = job.g;
+  const int m = g.m, n = g.n, nbm = (m + C::BM - 1) / C::BM, nbn = (n + C::BN - 1) / C::BN;
+  // An XCD gets a contiguous range of the tiles of every job: of all of them together, the long contractions of one job would all be on a few XCDs.
+  int local = blockIdx.x - d.first_block[ji];
+  const int per_xcd = (d.first_block[ji + 1] - d.first_block[ji]) >> 3;
+  if (local < 8 * per_xcd) local = (local & 7) * per_xcd + (local >> 3);
+  const int per = SYMM ? nbm * (nbm + 1) / 2 : nbm * nbn, mat = local / per, t = local % per;
+  int ti, tj;
+  if (SYMM) upper_tile(t, nbm, ti, tj);
+  else tile_of_block<4>(t, nbn, nbm, ti, tj);
+  ti = __builtin_amdgcn_readfirstlane(ti); tj = __builtin_amdgcn_readfirstlane(tj);
+  const int m0 = ti * C::BM, n0 = tj * C::BN;
+  constexpr int split = SPLIT ? 1 : 0;
+  char* const base = d.ws + g.ws + mat * g.stride;
+  f16* const X = (f16*)(base + d.from * x_bytes(g));
+  f16* const Xn = (f16*)(base + (d.from ^ 1) * x_bytes(g));
+
+  // operands, and how far behind the first numbers the second ones are (bytes)
+  const f16* const opA = OP == NS_GRAM ? X : buf_ptr(base, g, split, job.p);
+  const f16* const opB = OP == NS_SYM ? buf_ptr(base, g, split, job.q) : X;
+  const int K = OP == NS_GRAM ? n : m;
+  const int64_t sizeA = (int64_t)m * K * 2, sizeB = OP == NS_SYM ? sizeA : (int64_t)m * n * 2;
+  const int nk1 = K / 64, nseg = split ? 3 : 1;
+  typename TA::Cursor ca;
+  typename TB::Cursor cb;
+  TA::init(ca, (const bf16*)opA, K, m0, m, 0, K, lane, lw);
+  if (SYMM) TB::init(cb, (const bf16*)opB, K, n0, m, 0, K, lane, lw);
+  else TB::init(cb, (const bf16*)opB, n, n0, n, 0, K, lane, lw);
+  ca.rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)opA, 0, (int)(split ? 2 * sizeA : sizeA), 0x00020000);
+  cb.rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)opB, 0, (int)(split ? 2 * sizeB : sizeB), 0x00020000);
+  // k-tiles of the products hi hi, hi lo, lo hi one behind the other; then behind the operands
+  auto from = [&](int seg, int kt) __attribute__((always_inline)) {
+    ca.soff = seg >= nseg ? 0x80000000u : (seg == 2 ? (unsigned)sizeA : 0u) + kt * ca.step;
+    cb.soff = seg >= nseg ? 0x80000000u : (seg == 1 ? (unsigned)sizeB : 0u) + kt * cb.step;
+  };
+  // Way out: a wave's 32-row slabs go through LDS, from where a lane takes 8 columns of a row (the same columns in every slab).  What a slab needs from memory is
+  // requested while the one before it is worked on.  The mirror image comes out of a second copy of the slab, of the fp16 numbers that were
+  // written, by transposing reads: 16 lanes get 16 columns, each 8 rows of one (and the four groups of 16 lanes the 32 rows).
+  const int rbase = m0 + wm * TI * 32, cbase = n0 + wn * TJ * 32;
+  const int ldo = SYMM ? m : n;                                     // of what is written, and of what it is added to
+  const bool inside = rbase + 32 * TI <= m && cbase + WN <= ldo;    // sides are multiples of 64, so a slab of 8 is in or out as a whole
+  constexpr int LDH = WN + 8;                                       // of the copy, in fp16 numbers
+  float* const stage = (float*)(lds_raw + lw * ns_wave_bytes<C, OP, SPLIT>());
+  f16* const half = (f16*)(stage + C::EPI_FLOATS);
+  const bool mirror = SYMM && ti != tj;
+  f16* const out = SYMM ? buf_ptr(base, g, split, job.out) : Xn;
+  const int64_t lo_at = (int64_t)m * ldo;                           // second numbers
+  float* const dout = SYMM ? diag_ptr(base, g, split, job.out) : nullptr;
+  const float* const dp = OP == NS_GRAM ? nullptr : diag_ptr(base, g, split, job.p);
+  const f16* const auxp = OP == NS_SYM ? opA : X;
+  const f16* const auxq = opB;
+  const bool same = OP == NS_SYM && job.p == job.q;
+  const float f_out = SYMM ? buf_scale(job.out) : OP == NS_LAST ? 1.0f / kSx : 1.0f;
+  const float f_acc = f_out * (OP == NS_GRAM ? 1.0f / (kSx * kSx) : OP == NS_SYM ? job.beta / (buf_scale(job.p) * buf_scale(job.q)) : 1.0f / buf_scale(job.p));
+  // SYM, off the diagonal: out = f_acc acc + (rp + cp[column]) E_P + rq(row) E_Q, where for P = Q both go to E_P
+  const float f_p = OP == NS_SYM ? f_out / buf_scale(job.p) : 0.0f, f_q = OP == NS_SYM ? f_out / buf_scale(job.q) : 0.0f;
+  const int lane_col = cbase + (lane % (WN / 8)) * 8;
+  float cp[8];
+  if (OP == NS_SYM) {
+    const float* const dq = diag_ptr(base, g, split, job.q);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) cp[k] = lane_col < m ? f_p * (job.alpha + job.beta * dq[lane_col + k]) : 0.0f;
+  }
+  const NsPlace at = OP == NS_LAST ? d.table[g.first + mat] : NsPlace{0, 0};
+  const bool quads = ((at.offset | at.ld) & 3) == 0;                // rows of the flat buffers start on 16 bytes
+  float step = 0.0f;
+  if constexpr (UPDATE)
+    step = io.lr * (io.rms > 0.0f ? io.rms * sqrtf((float)max(g.rows, g.cols)) : sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)));
+
+  // 8 neighbours of a row of the flat buffers, `have` of which exist; w: their weights, loaded before
+  auto load_w = [&](int64_t i, bool whole, float (&w)[8]) __attribute__((always_inline)) {
+    if constexpr (UPDATE) {
+      if (whole) {
+        const float4 a = *(const float4*)(io.w + i), b = *(const float4*)(io.w + i + 4);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+      }
+    }
+  };
+  auto emit = [&](int64_t i, int have, bool whole, float (&w)[8], const float (&y)[8]) __attribute__((always_inline)) {
+    if constexpr (UPDATE) {
+      if (whole) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = io.decay * w[k] - step * y[k];
+        *(float4*)(io.w + i) = make_float4(w[0], w[1], w[2], w[3]);
+        *(float4*)(io.w + i + 4) = make_float4(w[4], w[5], w[6], w[7]);
+        if (io.wl) {
+          bf16x4 a, b;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) { a[k] = (bf16)w[k]; b[k] = (bf16)w[k + 4]; }
+          *(bf16x4*)(io.wl + i) = a;
+          *(bf16x4*)(io.wl + i + 4) = b;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < have) {
+            const float x = io.decay * io.w[i + k] - step * y[k];
+            io.w[i + k] = x;
+            if (io.wl) io.wl[i + k] = (bf16)x;
+          }
+      }
+    } else if constexpr (OP == NS_LAST) {
+      if (io.bf) {
+        bf16* const o = (bf16*)io.y + i;
+        if (whole) {
+          bf16x4 a, b;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) { a[k] = (bf16)y[k]; b[k] = (bf16)y[k + 4]; }
+          *(bf16x4*)o = a;
+          *(bf16x4*)(o + 4) = b;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) if (k < have) o[k] = (bf16)y[k];
+        }
+      } else {
+        float* const o = (float*)io.y + i;
+        if (whole) {
+          *(float4*)o = make_float4(y[0], y[1], y[2], y[3]);
+          *(float4*)(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) if (k < have) o[k] = y[k];
+        }
+      }
+    }
+  };
+
+  auto place = [&](int it, int& lr, int& lc) __attribute__((always_inline)) {
+    const int piece = it * 64 + lane;
+    lr = piece / (WN / 8); lc = (piece % (WN / 8)) * 8;
+  };
+  auto place_t = [&](int it, int& lr, int& lc) __attribute__((always_inline)) {      // a tall matrix' way out: row group, column
+    const int piece = it * 64 + lane;
+    lr = (piece & 3) * 8; lc = piece >> 2;
+  };
+  // where 8 values go in the flat buffers, and how many of them there are
+  auto target = [&](int i, int lr, int lc, int64_t& o, int& have) __attribute__((always_inline)) {
+    const int row = rbase + i * 32 + lr, col = cbase + lc;
+    if (g.tall) { o = at.offset + (int64_t)col * at.ld + row; have = col < g.rows ? g.cols - row : 0; }
+    else { o = at.offset + (int64_t)row * at.ld + col; have = row < g.rows ? g.cols - col : 0; }
+  };
+  struct Aux { f16x8 p[NIT], pl[NIT], q[NIT], ql[NIT]; float d[NIT], dq[NIT], w[OP == NS_LAST ? NIT : 1][8]; };
+  auto request = [&](auto all_tag, Aux& a, int i) __attribute__((always_inline)) {
+    constexpr bool ALL = decltype(all_tag)::value;      // no piece is outside
+    if (OP != NS_GRAM) {
+#pragma unroll
+      for (int it = 0; it < NIT; ++it) {
+        int lr, lc;
+        place(it, lr, lc);
+        const int row = rbase + i * 32 + lr, col = cbase + lc;
+        if (!ALL && (row >= m || col >= ldo)) continue;
+        const int64_t o = (int64_t)row * ldo + col;
+        a.p[it] = *(const f16x8*)(auxp + o);
+        if (!SYMM || SPLIT) a.pl[it] = *(const f16x8*)(auxp + lo_at + o);
+        if (OP == NS_SYM && !same) {
+          a.q[it] = *(const f16x8*)(auxq + o);
+          if (SPLIT) a.ql[it] = *(const f16x8*)(auxq + lo_at + o);
+        }
+        a.d[it] = dp[row];
+        if (OP == NS_SYM) a.dq[it] = diag_ptr(base, g, split, job.q)[row];
+      }
+    }
+    if constexpr (OP == NS_LAST) {
+#pragma unroll
+      for (int it = 0; it < NIT; ++it) {
+        int lr, lc, have;
+        int64_t o;
+        if (g.tall) place_t(it, lr, lc); else place(it, lr, lc);
+        target(i, lr, lc, o, have);
+        load_w(o, quads && have >= 8, a.w[it]);
+      }
+    }
+  };
+  constexpr bool EARLY = !(UPDATE && TI > 2) && !(OP == NS_SYM && SPLIT);      // room in registers for two slabs' requests
+  Aux aux[EARLY ? 2 : 1];
+
+  f32x16 acc[TI][TJ];
+  clear_tiles(acc);
+  int sa[TI] = {}, sb[TJ] = {}, seg = 0;
+  if constexpr (KSPLIT) {
+    int kt = wave;
+    auto next = [&](unsigned char* dst) __attribute__((always_inline)) {
+      while (kt >= nk1 && seg < nseg) { kt -= nk1; ++seg; }
+      from(seg, kt);
+      kt += C::KW;
+      TA::issue(ca, dst, 0);
+      TB::issue(cb, dst + TA::BYTES, 0);
+    };
+    const int nk = nk1 * nseg;
+    ks_loop<MmaF16, TA, TB, C::KW, C::S>(nk > wave ? (nk - wave + C::KW - 1) / C::KW : 0, lds_raw, acc[0][0], sa[0], sb[0], lane, wave, next, [](int) {});
+    if (wave > 0) return;
+  } else {
+    int kt = 0;
+    auto next = [&](unsigned char* dst) __attribute__((always_inline)) {
+      if (kt == nk1) { kt = 0; from(++seg, 0); }
+      ++kt;
+      TA::issue(ca, dst, wave);
+      TB::issue(cb, dst + TA::BYTES, wave);
+    };
+    mma_loop<C, MmaF16, TA, TB>(nk1 * nseg, lds_raw, acc, sa, sb, wm, wn, lane, next, [](int) {});
+  }
+
+  auto flow = [&](auto all_tag) __attribute__((always_inline)) {
+    constexpr bool ALL = decltype(all_tag)::value;
+    auto slab = [&](Aux& a, int i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) stage[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * LDW + j * 32 + (lane & 31)] = acc[i][j][r];
+#pragma unroll
+      for (int it = 0; it < NIT; ++it) {
+        int lr, lc;
+        place(it, lr, lc);
+        const int row = rbase + i * 32 + lr, col = cbase + lc;
+        if (!ALL && (row >= m || col >= ldo)) continue;
+        const int64_t o = (int64_t)row * ldo + col;
+        float* const st = stage + lr * LDW + lc;
+        const float4 s0 = *(const float4*)st, s1 = *(const float4*)(st + 4);
+        const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+        float x[8];
+        if (OP == NS_GRAM) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) x[k] = s[k] * f_acc;
+        } else if (OP == NS_SYM) {
+          const float rq = job.beta * a.d[it];
+          const float rp = same ? rq * f_p : 0.0f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            float e = (float)a.p[it][k];
+            if (SPLIT) e += (float)a.pl[it][k];
+            x[k] = s[k] * f_acc + (cp[k] + rp) * e;
+          }
+          if (!same) {
+            const float f = rq * f_q;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float e = (float)a.q[it][k];
+              if (SPLIT) e += (float)a.ql[it][k];
+              x[k] += f * e;
+            }
+          }
+        } else {
+          const float f = a.d[it] * f_out;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) x[k] = f * ((float)a.p[it][k] + (float)a.pl[it][k]) + s[k] * f_acc;
+        }
+        if (SYMM && row / 8 == col / 8) {      // the diagonal goes apart
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (row == col + k) {
+              if (OP == NS_GRAM) dout[row] = x[k] * (1.0f / f_out);
+              else dout[row] = job.ident + job.alpha * a.d[it] + job.beta * a.d[it] * a.dq[it] + s[k] * (f_acc / f_out);
+              x[k] = 0.0f;
+            }
+        }
+        if (OP == NS_LAST) {
+          if (!g.tall) {
+            int64_t to;
+            int have;
+            target(i, lr, lc, to, have);
+            emit(to, have, quads && have >= 8, a.w[OP == NS_LAST ? it : 0], x);
+          } else {
+            *(float4*)st = make_float4(x[0], x[1], x[2], x[3]);
+            *(float4*)(st + 4) = make_float4(x[4], x[5], x[6], x[7]);
+          }
+        } else {
+          f16x8 h;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) h[k] = (f16)x[k];
+          *(f16x8*)(out + o) = h;
+          if (mirror) *(f16x8*)(half + lr * LDH + lc) = h;
+          if (!SYMM || SPLIT) {
+            f16x8 l;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) l[k] = (f16)(x[k] - (float)h[k]);
+            *(f16x8*)(out + lo_at + o) = l;
+            if (mirror) *(f16x8*)(half + (32 + lr) * LDH + lc) = l;
+          }
+        }
+      }
+      if (mirror) {
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) {
+          const int lr = (lane >> 4) * 8, row = rbase + i * 32 + lr, col = cbase + it * 16 + (lane & 15);
+          if (!ALL && (row >= m || cbase + it * 16 >= m)) continue;
+          typedef s16x4 __attribute__((address_space(3))) * lds_v4;
+          const f16* const src = half + (lr + ((lane & 15) >> 2)) * LDH + it * 16 + 4 * (lane & 3);
+#pragma unroll
+          for (int part = 0; part < (SPLIT ? 2 : 1); ++part) {
+            union { struct { s16x4 a, b; } p; f16x8 v; } u;
+            u.p.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4)(src + part * 32 * LDH));
+            u.p.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4)(src + part * 32 * LDH + 4 * LDH));
+            *(f16x8*)(out + part * lo_at + (int64_t)col * m + row) = u.v;
+          }
+        }
+      }
+      if constexpr (OP == NS_LAST) {
+        if (g.tall) {
+#pragma unroll
+          for (int it = 0; it < NIT; ++it) {
+            int lr, lc, have;
+            int64_t o;
+            place_t(it, lr, lc);
+            target(i, lr, lc, o, have);
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = stage[(lr + k) * LDW + lc];
+            emit(o, have, quads && have >= 8, a.w[it], x);
+          }
+        }
+      }
+    };
+    if (EARLY) request(all_tag, aux[0], 0);
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      if (EARLY) { if (i + 1 < TI) request(all_tag, aux[EARLY ? (i + 1) & 1 : 0], i + 1); }
+      else request(all_tag, aux[0], i);
+      slab(aux[EARLY ? i & 1 : 0], i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (inside) flow(std::true_type{}); else flow(std::false_type{});
+}
+
+typedef DmaCfg<1, 1, 1, 1, 4, 64, 4, 1, false> Ns32;      // TI TJ WGM WGN KW BK S OCC AHEAD
 typedef DmaCfg<1, 1, 2, 2, 1, 64, 3, 3, true> Ns64;
 typedef DmaCfg<2, 2, 2, 2, 1, 64, 2, 2, true> Ns128;
+typedef DmaCfg<4, 2, 2, 4, 1, 64, 2, 1, true> Ns256;
 
 int64_t ns_tiles(const NsGroup& g, int op, int bm, int bn) {
   const int64_t nbm = (g.m + bm - 1) / bm, nbn = (g.n + bn - 1) / bn;
-  return g.count * (op == NS_GRAM || op == NS_SQUARE ? nbm * (nbm + 1) / 2 : nbm * nbn);
+  return g.count * (op == NS_GRAM || op == NS_SYM ? nbm * (nbm + 1) / 2 : nbm * nbn);
 }
 
-template <class C, int OP, class IO>
-hipError_t launch_product(NsDev d, const IO& io, hipStream_t s) {
+constexpr int kCUs = 256;
+struct NoIO {};
+template <class C, int OP, bool SPLIT, class IO>
+hipError_t launch_product(NsDev& d, const IO& io, hipStream_t s) {
   int64_t blocks = 0;
-  for (int i = 0; i < d.ng; ++i) { d.first_block[i] = (int)blocks; blocks += ns_tiles(d.g[i], OP, C::BM, C::BN); }
-  d.first_block[d.ng] = (int)blocks;
-  auto kern = ns_product_kernel<C, OP, IO>;
-  if (C::LDS > 48 * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
+  for (int i = 0; i < d.n; ++i) { d.first_block[i] = (int)blocks; blocks += ns_tiles(d.job[i].g, OP, C::BM, C::BN); }
+  d.first_block[d.n] = (int)blocks;
+  auto kern = ns_product_kernel<C, OP, SPLIT, IO>;
+  constexpr size_t lds = ns_lds<C, OP, SPLIT>();
+  static_assert(C::OCC * lds <= 160 * 1024, "the blocks of a CU do not fit its LDS");
+  static bool configured = false;      // per instantiation, as in gemm_wide.h
+  if (!configured && lds > 48 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(C::NT), C::LDS, s, d, io);
+  configured = true;
+  hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(C::NT), lds, s, d, io);
   return hipGetLastError();
 }
 template <int OP, class IO>
-hipError_t product(const NsDev& d, const IO& io, hipStream_t s) {
-  int64_t t128 = 0;
-  for (int i = 0; i < d.ng; ++i) t128 += ns_tiles(d.g[i], OP, 128, 128);
-  return t128 >= 192 ? launch_product<Ns128, OP, IO>(d, io, s) : launch_product<Ns64, OP, IO>(d, io, s);
+hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
+  // Rounds that the tiles of a size take on the chip (one 256 x 256 tile per CU, two of 128 x 128, three of 64 x 64) times what a round takes, as a share of one
+  // of 256 x 256 tiles, from lists of 48 and 96 matrices of 1024 x 1024 and 1024 x 4096 (us with 256, 128, 64: GRAM 171, 189, 219; SYM 216, 211, 242; APPLY
+  // 303, 335, 466).  256 x 256 tiles are not built for 32-bit products.
+  constexpr float kRound128 = OP == NS_SYM ? 0.48f : 0.55f, kRound64 = OP == NS_SYM ? 0.21f : OP == NS_GRAM ? 0.24f : 0.28f;
+  auto rounds = [&](int b, int slots) {
+    int64_t tiles = 0;
+    for (int i = 0; i < d.n; ++i) tiles += ns_tiles(d.job[i].g, OP, b, b);
+    return (float)((tiles + slots - 1) / slots);
+  };
+  int64_t t32 = 0;
+  for (int i = 0; i < d.n; ++i) t32 += ns_tiles(d.job[i].g, OP, 32, 32);
+  if (t32 <= kCUs) return d.split ? launch_product<Ns32, OP, true, IO>(d, io, s) : launch_product<Ns32, OP, false, IO>(d, io, s);
+  const float t256 = rounds(256, kCUs), t128 = rounds(128, 2 * kCUs) * kRound128, t64 = rounds(64, 3 * kCUs) * kRound64;
+  if (d.split) return t128 <= t64 ? launch_product<Ns128, OP, true, IO>(d, io, s) : launch_product<Ns64, OP, true, IO>(d, io, s);
+  if constexpr (OP != NS_SYM) { if (t256 <= std::min(t128, t64)) return launch_product<Ns256, OP, false, IO>(d, io, s); }
+  return t128 <= t64 ? launch_product<Ns128, OP, false, IO>(d, io, s) : launch_product<Ns64, OP, false, IO>(d, io, s);
 }
+
+// A matrix whose longer side is at least twice the shorter is better served by polynomials of A than by products with X: over up to three steps
+// X <- S_3 S_2 S_1 X with S_i = a I + b A_i + c A_i A_i and A_(i+1) = S_i A_i S_i, all symmetric m x m matrices that commute, and X itself is read
+// and written once.  Five steps are 6 m m n + 14 m m m operations instead of 15 m m n + 5 m m m, in 17 launches instead of 15, beside those of the matrices that stay with the
+// other form.  Where that pays (us, with and without): of a list by itself from 1.5e10 operations saved on (16 of 256 x 2048: 179, 191; 4: 156, 147), in a
+// stack of layers with square matrices from 8e10 on (12 layers of hidden 512: 1037, 1082; 3 of 768: 723, 699; 24 of 1024: 8.6 ms, 10.1 ms).
+constexpr double kGramAlone = 1.5e10, kGramBeside = 8e10;
 
 // The shapes of a list and the order of its matrices, shape by shape; the workspace is laid out as [table][partial sums][matrices].
 struct NsPlan {
@@ -370,7 +642,9 @@ NsPlan ns_plan(const hs_matrix* mats, int n, int split) {
   p.order.resize(n);
   std::iota(p.order.begin(), p.order.end(), 0);
   std::stable_sort(p.order.begin(), p.order.end(), [&](int i, int j) {
-    return mats[i].rows != mats[j].rows ? mats[i].rows > mats[j].rows : mats[i].cols > mats[j].cols;
+    const int si = std::min(mats[i].rows, mats[i].cols), li = std::max(mats[i].rows, mats[i].cols);
+    const int sj = std::min(mats[j].rows, mats[j].cols), lj = std::max(mats[j].rows, mats[j].cols);
+    return std::make_tuple(lj, sj, mats[j].rows) < std::make_tuple(li, si, mats[i].rows);      // long contractions first
   });
   p.table = 0;
   p.partial = align_up((size_t)n * sizeof(NsPlace), 256);
@@ -384,10 +658,20 @@ NsPlan ns_plan(const hs_matrix* mats, int n, int split) {
     g.m = (std::min(a.rows, a.cols) + 63) / 64 * 64; g.n = (std::max(a.rows, a.cols) + 63) / 64 * 64;
     g.count = j - i; g.first = i;
     g.parts = (int)std::min<int64_t>(kParts, ((int64_t)a.rows * a.cols + kPartElems - 1) / kPartElems);
-    g.ws = (int64_t)off; g.stride = (int64_t)ns_parts(g.m, g.n, split).total;
-    off += (size_t)g.stride * g.count;
     p.groups.push_back(g);
     i = j;
+  }
+  double saved = 0.0;
+  bool others = false;
+  for (const NsGroup& g : p.groups) {
+    if (!split && g.n >= 2 * g.m) saved += 9.0 * g.m * (double)g.m * (g.n - g.m) * g.count;
+    else others = true;
+  }
+  const bool gram = saved >= (others ? kGramBeside : kGramAlone);
+  for (NsGroup& g : p.groups) {
+    g.bufs = gram && g.n >= 2 * g.m ? BUFS : BUF_S + 1;
+    g.ws = (int64_t)off; g.stride = (int64_t)matrix_bytes(g, split);
+    off += (size_t)g.stride * g.count;
   }
   p.total = off;
   return p;
@@ -426,6 +710,69 @@ bool ns_disjoint(const hs_matrix* mats, int n) {
   return true;
 }
 
+// The whole of it for groups that go through the same products.
+template <class IO>
+hipError_t ns_run(const std::vector<NsGroup>& groups, bool gram, int split, char* ws, const NsPlace* table, double* partial, const IO& io, int steps,
+                  const double* c, double eps, hipStream_t s) {
+  NsDev d{};
+  d.split = split; d.ws = ws; d.table = table; d.partial = partial;
+  auto add = [&](int p, int q, int out, double ident, double alpha, double beta) {
+    for (const NsGroup& g : groups) d.job[d.n++] = NsJob{g, p, q, out, (float)ident, (float)alpha, (float)beta};
+  };
+  auto blocks_of = [&](auto per) {
+    int64_t blocks = 0;
+      for (int i = 0; i < d.n; ++i) { d.first_block[i] = (int)blocks; blocks += (int64_t)d.job[i].g.count * per(d.job[i].g); }
+    d.first_block[d.n] = (int)blocks;
+    return (unsigned)blocks;
+  };
+  add(0, 0, 0, 0.0, 0.0, 0.0);
+  unsigned blocks = blocks_of([](const NsGroup& g) { return g.parts; });
+  hipLaunchKernelGGL(ns_norm_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io);
+  blocks = blocks_of([](const NsGroup& g) { return (g.m / 64) * (g.n / 64); });
+  hipLaunchKernelGGL(ns_start_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io, eps);
+  hipError_t e = hipGetLastError();
+  auto go = [&](auto op) {
+    constexpr int OP = decltype(op)::value;
+    if (e == hipSuccess && d.n > 0) {
+      if constexpr (OP == NS_LAST) e = product<OP, IO>(d, io, s); else e = product<OP, NoIO>(d, NoIO{}, s);
+    }
+    d.n = 0;
+  };
+  typedef std::integral_constant<int, NS_GRAM> Gram;
+  typedef std::integral_constant<int, NS_SYM> Sym;
+  d.n = 0;
+  for (int k = 0; k < steps && e == hipSuccess;) {
+    // steps taken on A alone: their product must stay in range of its buffer
+    int len = 1;
+    double grown = std::fabs(c[3 * k]);
+    while (gram && len < 3 && k + len < steps && (grown *= std::fabs(c[3 * (k + len)])) <= 64.0) ++len;
+    add(0, 0, BUF_A, 0.0, 0.0, 1.0);
+    go(Gram{});
+    int q = BUF_S;      // the product of the steps so far
+    for (int j = 0; j < len; ++j) {
+      const int out = j == 0 && len > 1 ? BUF_Q : BUF_S;
+      add(BUF_A, BUF_A, out, c[3 * (k + j)], c[3 * (k + j) + 1], c[3 * (k + j) + 2]);
+      go(Sym{});
+      if (j + 1 < len) add(out, BUF_A, BUF_T, 0.0, 0.0, 1.0);
+      if (j == 0) {
+        q = out;
+      } else {
+        const int to = q == BUF_Q ? BUF_Q2 : BUF_Q;
+        add(BUF_S, q, to, 0.0, 0.0, 1.0);
+        q = to;
+      }
+      go(Sym{});
+      if (j + 1 < len) add(BUF_T, out, BUF_A, 0.0, 0.0, 1.0);
+      go(Sym{});
+    }
+    k += len;
+    add(q, 0, 0, 0.0, 0.0, 1.0);
+    if (k < steps) go(std::integral_constant<int, NS_APPLY>{}); else go(std::integral_constant<int, NS_LAST>{});
+    d.from ^= 1;
+  }
+  return e;
+}
+
 const double kDefaultCoeff[3] = {3.4445, -4.7750, 2.0315};
 
 template <class IO>
@@ -460,30 +807,14 @@ hs_status orthogonalize(const char* who, const IO& io, size_t size, const hs_mat
     hipLaunchKernelGGL(ns_table_kernel, dim3(1), dim3(256), 0, s, t, table);
     e = hipGetLastError();
   }
-  for (size_t g0 = 0; g0 < plan.groups.size() && e == hipSuccess; g0 += kGroups) {
-    NsDev d{};
-    d.ng = (int)std::min<size_t>(kGroups, plan.groups.size() - g0);
-    for (int i = 0; i < d.ng; ++i) d.g[i] = plan.groups[g0 + i];
-    d.split = split; d.ws = ws; d.table = table; d.partial = (double*)(ws + plan.partial); d.from = 0;
-    auto blocks_of = [&](auto per) {
-      int64_t blocks = 0;
-      for (int i = 0; i < d.ng; ++i) { d.first_block[i] = (int)blocks; blocks += (int64_t)d.g[i].count * per(d.g[i]); }
-      d.first_block[d.ng] = (int)blocks;
-      return (unsigned)blocks;
-    };
-    unsigned blocks = blocks_of([](const NsGroup& g) { return g.parts; });
-    hipLaunchKernelGGL(ns_norm_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io);
-    blocks = blocks_of([](const NsGroup& g) { return (g.m / 64) * (g.n / 64); });
-    hipLaunchKernelGGL(ns_start_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io, eps);
-    e = hipGetLastError();
-    for (int k = 0; k < steps && e == hipSuccess; ++k) {
-      const double* const c = coeff ? coeff + 3 * k : kDefaultCoeff;
-      d.a = (float)c[0]; d.b = (float)c[1]; d.c = (float)c[2];
-      e = product<NS_GRAM>(d, io, s);
-      if (e == hipSuccess) e = product<NS_SQUARE>(d, io, s);
-      if (e == hipSuccess) e = k + 1 < steps ? product<NS_APPLY>(d, io, s) : product<NS_LAST>(d, io, s);
-      d.from ^= 1;
-    }
+  std::vector<double> c(3 * steps);
+  for (int k = 0; k < 3 * steps; ++k) c[k] = coeff ? coeff[k] : kDefaultCoeff[k % 3];
+  // runs of groups that go through the same products, as many as the jobs of a launch
+  for (size_t g0 = 0; g0 < plan.groups.size() && e == hipSuccess;) {
+    std::vector<NsGroup> now;
+    const bool gram = plan.groups[g0].bufs == BUFS;
+    for (; g0 < plan.groups.size() && now.size() < kJobs / 2 && (plan.groups[g0].bufs == BUFS) == gram; ++g0) now.push_back(plan.groups[g0]);
+    e = ns_run(now, gram, split, ws, table, (double*)(ws + plan.partial), io, steps, c.data(), eps, s);
   }
   return e == hipSuccess ? HS_OK : hs_fail(nullptr, HS_ERR_HIP, name + hipGetErrorString(e));
 }

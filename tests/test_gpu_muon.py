@@ -22,14 +22,14 @@ def rel(a, b):
     return np.linalg.norm(a - b) / nb if nb > 0 else np.linalg.norm(a - b)
 
 
-def tolerance(x, products, **kw):
+def tolerance(x, products, runs=None, **kw):
     """What the kernels' roundings come to, by the oracle with the same ones: X kept as two numbers of 11 bits, operands of one (16-bit products) or two, 32-bit
     sums.  (The sums have to be in it: 513 in 32-bit products are 97 additions of up to 2^-24 of the running sum each, which together are more than the
     2^-23 of a number kept in 22 bits.)  Twice that, for sums in another order; at least 8 of 22 bits.  Roundings that fall otherwise: the
     error is that of k = min(rows, cols) directions, each of which its own amplification makes a sum of few, so both norms are samples of a
     distribution with k degrees of freedom, three of whose standard deviations are 3 / sqrt(2 k) of it; 3 / sqrt(k) for the two."""
     e = M.orthogonalize(x, **kw)
-    return max(2.0 * (1.0 + 3.0 / np.sqrt(min(x.shape))) * rel(M.orthogonalize(x, numbers=1 if products == 1 else 2, **kw), e), 8 * 2.0 ** -22), e
+    return max(2.0 * (1.0 + 3.0 / np.sqrt(min(x.shape))) * rel(M.orthogonalize(x, numbers=1 if products == 1 else 2, runs=runs, **kw), e), 8 * 2.0 ** -22), e
 
 
 def layout(shapes, gap=0, ld=0):
@@ -92,6 +92,39 @@ def test_larger_matrices(hs, products, shape, count):
     for mat in mats[:2] + mats[-1:]:
         tol, e = tolerance(view(x.astype(np.float64), mat), products)
         assert rel(view(got, mat), e) <= tol
+
+
+@pytest.mark.parametrize("shape,count,beside", [((500, 2100), 5, 0), ((2100, 500), 5, 0), ((64, 3000), 150, 0), ((512, 2048), 24, 3)])
+def test_long_matrices_by_polynomials_of_their_gram_matrix(hs, shape, count, beside):
+    """Lists whose long matrices go through runs of three and two steps, by themselves and with square ones beside them."""
+    mats, size = layout([shape] * count + [(200, 200)] * beside)
+    rng = np.random.default_rng(shape[0])
+    x = gaussian(rng, size)
+    low = view(x, mats[0])      # one of low rank with noise
+    r = min(shape) // 16
+    low[...] = gaussian(rng, (shape[0], r)) @ gaussian(rng, (r, shape[1])) + 0.05 * low
+    y = torch.empty(size, device="cuda")
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, 1)
+    hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, size, lst, 1, 5, None, 1e-7, ws, n)
+    got = y.cpu().double().numpy()
+    for mat in mats[:2] + mats[count - 1:count + 1]:
+        tol, e = tolerance(view(x.astype(np.float64), mat), 1, runs=(3, 2) if mat[2:] == shape else None)
+        assert tol < 1e-2 and rel(view(got, mat), e) <= tol, mat
+
+
+@pytest.mark.parametrize("steps,coeff,runs", [(1, None, (1,)), (2, None, (2,)), (4, None, (3, 1)), (3, [(9.0, -8.0, 1.0), (8.0, -6.0, 1.0), (1.5, -0.5, 0.0)], (1, 2))])
+def test_other_steps_by_the_gram_matrix(hs, steps, coeff, runs):
+    """Runs end where the steps do, and where the product of their first coefficients would pass 64 (9 * 8 does, 8 * 1.5 does not)."""
+    shape, count = (500, 2100), 5
+    mats, size = layout([shape] * count)
+    x = gaussian(np.random.default_rng(steps), size)
+    y = torch.empty(size, device="cuda")
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, 1)
+    hs.hs_op_orthogonalize(0, torch.from_numpy(x).cuda(), y, size, lst, 1, steps, coeff, 1e-7, ws, n)
+    tol, e = tolerance(view(x.astype(np.float64), mats[2]), 1, runs=runs, steps=steps, coeff=coeff)
+    assert rel(view(y.cpu().double().numpy(), mats[2]), e) <= tol
 
 
 @pytest.mark.parametrize("products", [0, 1])

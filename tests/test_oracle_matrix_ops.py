@@ -75,6 +75,16 @@ def test_emulated_roundings_shrink_with_the_numbers():
         assert 1e-4 < off[0] < 4e-3 and 1e-7 < off[1] < 1e-5
 
 
+def test_runs_of_steps_on_the_gram_matrix_are_the_same_polynomial():
+    """The runs' own roundings apart: a few times those of the steps one by one."""
+    x = np.random.default_rng(7).standard_normal((30, 90))
+    e = M.orthogonalize(x)
+    for runs in ((1, 1, 1, 1, 1), (2, 2, 1), (3, 2)):
+        for n, most in ((1, 1e-2), (2, 1e-4)):
+            off = np.linalg.norm(M.orthogonalize(x, numbers=n, runs=runs) - e) / np.linalg.norm(e)
+            assert 0 < off < most
+
+
 def test_update_of_one_matrix_by_hand():
     w, m, G = np.array([[1.0]]), np.array([[2.0]]), np.array([[6.0]])
     nw, nm, O = M.muon_step(w, m, G, lr=0.1, momentum=0.5, weight_decay=0.2, rms=0.0, denom=3.0, steps=1, eps=0.0)
