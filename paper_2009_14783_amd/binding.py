@@ -147,17 +147,16 @@ def _ptr(t):
     """Device/host address of a torch tensor or numpy array (None -> NULL)."""
     if t is None:
         return None
-    if isinstance(t, np.ndarray):
-        return t.ctypes.data
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
+    try:
+        return t.data_ptr()      # tensors first: a call passes up to nine of them
+    except AttributeError:
+        return t.ctypes.data if isinstance(t, np.ndarray) else t
 
 
 def _stream(stream):
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())      # torch.cuda.current_stream().cuda_stream without its objects: 0.3 us, 2.7
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -46,28 +46,18 @@ struct QuantDev {
   int nbx;                         // blocks along the columns
 };
 
+// A thread's 8 columns of the block's 128: neighbours in bf16, two times four in fp32, so that 16 lanes read whole lines with 16 bytes each.
 template <class T>
-__device__ __forceinline__ void load8(const T* __restrict__ p, int n, bool vec, float (&v)[8]);
-template <>
-__device__ __forceinline__ void load8<float>(const float* __restrict__ p, int n, bool vec, float (&v)[8]) {
-  if (vec && n >= 8) {
-    const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = t < n ? p[t] : 0.0f;
-  }
+__device__ __forceinline__ int quant_col(int cg, int t) { return sizeof(T) == 2 ? cg * 8 + t : (t >> 2) * 64 + cg * 4 + (t & 3); }
+// half h of them (bf16: all, half 0), from their first
+__device__ __forceinline__ void load_half(const float* __restrict__ p, int h, float (&v)[8]) {
+  const float4 a = *(const float4*)p;
+  v[4 * h] = a.x; v[4 * h + 1] = a.y; v[4 * h + 2] = a.z; v[4 * h + 3] = a.w;
 }
-template <>
-__device__ __forceinline__ void load8<bf16>(const bf16* __restrict__ p, int n, bool vec, float (&v)[8]) {
-  if (vec && n >= 8) {
-    const bf16x8 a = *(const bf16x8*)p;
+__device__ __forceinline__ void load_half(const bf16* __restrict__ p, int, float (&v)[8]) {
+  const bf16x8 a = *(const bf16x8*)p;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = (float)a[t];
-  } else {
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = t < n ? (float)p[t] : 0.0f;
-  }
+  for (int t = 0; t < 8; ++t) v[t] = (float)a[t];
 }
 
 template <class T>
@@ -79,14 +69,31 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_fp8_kernel(QuantDev p)
   const int64_t b = blockIdx.x;
   const int bc = (int)(b % p.nbx), br = (int)(b / p.nbx);
   const int cg = tid & 15, rg = tid >> 4;                // column group, row group (8 each)
-  const int c0 = bc * 128 + cg * 8, r0 = br * 128 + rg * 8;
-  const bool vec = (p.ldx % (16 / sizeof(T))) == 0 && ((uintptr_t)p.x & 15) == 0;
+  const int r0 = br * 128 + rg * 8;
+  // All loads of a thread are under way before the first is used: rows behind the matrix read its last one and become zeros afterwards.  (With a branch
+  // per row instead, 8192 x 4096 took 43 us in place of 32.)
+  constexpr int HALVES = sizeof(T) / 2, HALF = 8 / HALVES;
+  const bool vec = (p.ldx % HALF) == 0 && ((uintptr_t)p.x & 15) == 0;
   float v[8][8];
   const T* const src = (const T*)p.x;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + i;
-    load8<T>(src + (int64_t)r * p.ldx + c0, r < p.R ? p.C - c0 : 0, vec, v[i]);
+  for (int h = 0; h < HALVES; ++h) {
+    const int c = bc * 128 + quant_col<T>(cg, h * HALF);
+    if (vec && c + HALF <= p.C) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) load_half(src + (int64_t)min(r0 + i, p.R - 1) * p.ldx + c, h, v[i]);
+    } else if (c < p.C) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int t = 0; t < HALF; ++t) v[i][h * HALF + t] = (float)src[(int64_t)min(r0 + i, p.R - 1) * p.ldx + min(c + t, p.C - 1)];
+    }
+    if (r0 + 8 > p.R || c + HALF > p.C) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int t = 0; t < HALF; ++t) if (r0 + i >= p.R || c + t >= p.C) v[i][h * HALF + t] = 0.0f;
+    }
   }
   uint32_t rmax[8];
 #pragma unroll
@@ -120,7 +127,13 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_fp8_kernel(QuantDev p)
       uint2 o;
       o.x = codes4(scaled(v[i][0], inv), scaled(v[i][1], inv), scaled(v[i][2], inv), scaled(v[i][3], inv));
       o.y = codes4(scaled(v[i][4], inv), scaled(v[i][5], inv), scaled(v[i][6], inv), scaled(v[i][7], inv));
-      *(uint2*)(p.q + (int64_t)r * p.ldq + c0) = o;
+      uint8_t* const at = p.q + (int64_t)r * p.ldq + bc * 128;
+      if (sizeof(T) == 2) {
+        *(uint2*)(at + cg * 8) = o;
+      } else {
+        *(uint32_t*)(at + cg * 4) = o.x;
+        *(uint32_t*)(at + 64 + cg * 4) = o.y;
+      }
       if (cg == 0) p.qs[(int64_t)r * p.ldqs + bc] = (uint8_t)byte;
     }
   }
@@ -137,12 +150,12 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_fp8_kernel(QuantDev p)
       for (int i = 0; i < 8; ++i) m = max(m, finite_bits(v[i][t]));
       m = max(m, (uint32_t)__shfl_xor((int)m, 16));
       m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-      if (lane < 16) colmax[wave][cg * 8 + t] = m;
+      if (lane < 16) colmax[wave][quant_col<T>(cg, t)] = m;
     }
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-      const int c = cg * 8 + t;
+      const int c = quant_col<T>(cg, t);
       cbyte[t] = scale_byte(max(max(colmax[0][c], colmax[1][c]), max(colmax[2][c], colmax[3][c])));
     }
   }
@@ -152,8 +165,9 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_fp8_kernel(QuantDev p)
     uint2 o;
     o.x = codes4(scaled(v[0][t], inv), scaled(v[1][t], inv), scaled(v[2][t], inv), scaled(v[3][t], inv));
     o.y = codes4(scaled(v[4][t], inv), scaled(v[5][t], inv), scaled(v[6][t], inv), scaled(v[7][t], inv));
-    *(uint2*)(tq + (cg * 8 + t) * kQuantLd + rg * 8) = o;
-    if (rg == 0 && c0 + t < p.C) p.qts[(int64_t)(c0 + t) * p.ldqts + br] = (uint8_t)cbyte[t];
+    const int c = quant_col<T>(cg, t);
+    *(uint2*)(tq + c * kQuantLd + rg * 8) = o;
+    if (rg == 0 && bc * 128 + c < p.C) p.qts[(int64_t)(bc * 128 + c) * p.ldqts + br] = (uint8_t)cbyte[t];
   }
   __syncthreads();
 #pragma unroll
@@ -169,25 +183,50 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_fp8_kernel(QuantDev p)
 struct ScaleDev { const uint8_t *as, *bs; int64_t ldas, ldbs; };
 
 // C = sum over blocks kb of 2^(as[m, kb] - 127) 2^(bs[n, kb] - 127) sum over k in kb of A[m, k] B[n, k].  A k-tile is one block of 128 codes, so that a
-// lane's scales change with the k-tile: a row's bytes of four k-tiles are one word, read two groups ahead.  Both operands k-major, rows of whole k-tiles (zeros
+// row's scales of four k-tiles are one word; the words of the block's rows go into LDS like the operands, four k-tiles ahead, and from there into
+// registers (held there two groups ahead they would cost the 256 x 256 tile 18 registers that it does not have).  Both operands k-major, rows of whole k-tiles (zeros
 // behind K): nothing is masked.
+template <class C>
+constexpr size_t fp8_lds() { return std::max(C::PIPE, C::EPI_BYTES) + 2 * (C::BM + C::BN) * 4; }
+
 template <class C, class MMA>
 __device__ __forceinline__ void fp8_tile(const GemmDev& p, const ScaleDev& q, int m0, int n0, int split, unsigned char* lds_raw) {
   constexpr int TI = C::TI, TJ = C::TJ;
-  typedef DmaTile<true, C::BK, C::BM, C::NW> TA;
-  typedef DmaTile<true, C::BK, C::BN, C::NW> TB;
+  typedef DmaTile<true, C::BK, C::BM, C::NS> TA;
+  typedef DmaTile<true, C::BK, C::BN, C::NS> TB;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WGN, wn = wave % C::WGN;
   const int kbeg = split * p.k_per_split, kend = min(p.K, kbeg + p.k_per_split);
   const int nk = (kend - kbeg + 127) / 128;
   const int kbytes = (p.K + 127) / 128 * 128;
+  const int mrows = min(C::BM, p.M - m0), nrows = min(C::BN, p.N - n0);
   typename TA::Cursor ca;
   typename TB::Cursor cb;
   // in units of two bytes, from the tile's first row on: offsets of 32 bits reach over 256 rows
-  TA::init(ca, (const bf16*)p.A + (int64_t)m0 * (p.lda / 2), p.lda / 2, 0, min(C::BM, p.M - m0), kbeg / 2, kbytes / 2, lane, wave);
-  TB::init(cb, (const bf16*)p.B + (int64_t)n0 * (p.ldb / 2), p.ldb / 2, 0, min(C::BN, p.N - n0), kbeg / 2, kbytes / 2, lane, wave);
+  TA::init(ca, (const bf16*)p.A + (int64_t)m0 * (p.lda / 2), p.lda / 2, 0, mrows, kbeg / 2, kbytes / 2, lane, wave);
+  TB::init(cb, (const bf16*)p.B + (int64_t)n0 * (p.ldb / 2), p.ldb / 2, 0, nrows, kbeg / 2, kbytes / 2, lane, wave);
   f32x16 acc[TI][TJ];
   clear_tiles(acc);
+  const int words = (kbytes / 128 + 3) / 4;      // of a row of scales
+  int sa[TI], sb[TJ];
+  // the words of 64 rows per load instruction, A's rows first
+  constexpr int NB = (C::BM + C::BN) / 64, PER = (NB + C::NW - 1) / C::NW;
+  uint32_t* const store = (uint32_t*)(lds_raw + std::max(C::PIPE, C::EPI_BYTES));
+  const int64_t spanA = (int64_t)(mrows - 1) * q.ldas + 4 * words, spanB = (int64_t)(nrows - 1) * q.ldbs + 4 * words;
+  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)(q.as + (int64_t)m0 * q.ldas), 0, (int)spanA, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)(q.bs + (int64_t)n0 * q.ldbs), 0, (int)spanB, 0x00020000);
+  auto words_of = [&](int g) __attribute__((always_inline)) {      // group g of the split's k-tiles, into its half of the store
+    if (nk <= 0) return;
+    const int at = 4 * min(kbeg / 512 + g, words - 1);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int b = wave + k * C::NW;
+      uint32_t* const dst = store + (g & 1) * (C::BM + C::BN) + b * 64;
+      if (b < C::BM / 64) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_ptr)dst, 4, (int)(min(b * 64 + lane, mrows - 1) * (int)q.ldas), at, 0, 0);
+      else if (b < NB) __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_ptr)dst, 4, (int)(min(b * 64 + lane - C::BM, nrows - 1) * (int)q.ldbs), at, 0, 0);
+    }
+  };
+  words_of(0);
   int requested = 0;
   auto next = [&](unsigned char* dst) __attribute__((always_inline)) {
     if (requested >= nk) ca.soff = cb.soff = 0x80000000u;      // behind the operand: zeros
@@ -195,35 +234,13 @@ __device__ __forceinline__ void fp8_tile(const GemmDev& p, const ScaleDev& q, in
     TA::issue(ca, dst, wave);
     TB::issue(cb, dst + TA::BYTES, wave);
   };
-  const uint8_t *pa[TI], *pb[TJ];
-  uint32_t cura[TI], curb[TJ], nxta[TI], nxtb[TJ];
-  int sa[TI], sb[TJ];
-  const int first = kbeg / 512, lastg = (kbytes / 128 - 1) / 4;
-  auto word = [&](const uint8_t* row, int g) __attribute__((always_inline)) { return nk > 0 ? *(const uint32_t*)(row + 4 * g) : 0u; };      // none where K == 0
-#pragma unroll
-  for (int i = 0; i < TI; ++i) {
-    pa[i] = q.as + (int64_t)min(m0 + (wm * TI + i) * 32 + (lane & 31), p.M - 1) * q.ldas;
-    cura[i] = word(pa[i], first);
-    nxta[i] = word(pa[i], min(first + 1, lastg));
-  }
-#pragma unroll
-  for (int j = 0; j < TJ; ++j) {
-    pb[j] = q.bs + (int64_t)min(n0 + (wn * TJ + j) * 32 + (lane & 31), p.N - 1) * q.ldbs;
-    curb[j] = word(pb[j], first);
-    nxtb[j] = word(pb[j], min(first + 1, lastg));
-  }
   auto scales = [&](int t) __attribute__((always_inline)) {
-    if (t && (t & 3) == 0) {
-      const int g = min(first + (t >> 2) + 1, lastg);
+    const uint32_t* const src = store + ((t >> 2) & 1) * (C::BM + C::BN) + (lane & 31);
 #pragma unroll
-      for (int i = 0; i < TI; ++i) { cura[i] = nxta[i]; nxta[i] = word(pa[i], g); }
+    for (int i = 0; i < TI; ++i) sa[i] = (int)src[(wm * TI + i) * 32];
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) { curb[j] = nxtb[j]; nxtb[j] = word(pb[j], g); }
-    }
-#pragma unroll
-    for (int i = 0; i < TI; ++i) sa[i] = MMA::scale(cura[i], t);
-#pragma unroll
-    for (int j = 0; j < TJ; ++j) sb[j] = MMA::scale(curb[j], t);
+    for (int j = 0; j < TJ; ++j) sb[j] = (int)src[C::BM + (wn * TJ + j) * 32];
+    words_of((t >> 2) + 1);
   };
   mma_loop<C, MMA, TA, TB>(nk, lds_raw, acc, sa, sb, wm, wn, lane, next, scales);
 
@@ -249,20 +266,85 @@ void gemm_fp8_kernel(GemmDev p, ScaleDev q, int nbx, int nby) {
   fp8_tile<C, MMA>(p, q, tm * C::BM, tn * C::BN, split, lds_raw);
 }
 
-template <class C>
-hipError_t launch_fp8(const GemmDev& p, const ScaleDev& q, int splits, hipStream_t s) {
-  auto kern = p.c_f32 ? gemm_fp8_kernel<C, MmaE4M3Wide> : gemm_fp8_kernel<C, MmaE4M3>;
-  if (C::LDS > 48 * 1024) {
-    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
+template <class C, class MMA>
+hipError_t launch_fp8_one(const GemmDev& p, const ScaleDev& q, int splits, hipStream_t s) {
+  auto kern = gemm_fp8_kernel<C, MMA>;
+  constexpr size_t lds = fp8_lds<C>();
+  static_assert(C::OCC * lds <= 160 * 1024, "the blocks of a CU do not fit its LDS");
+  static bool configured = false;      // per instantiation, as in gemm_wide.h
+  if (!configured && lds > 48 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
+  configured = true;
   const int nbx = (p.N + C::BN - 1) / C::BN, nby = (p.M + C::BM - 1) / C::BM;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(nbx * nby * splits)), dim3(C::NT), C::LDS, s, p, q, nbx, nby);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(nbx * nby * splits)), dim3(C::NT), lds, s, p, q, nbx, nby);
   return hipGetLastError();
 }
+template <class C>
+hipError_t launch_fp8(const GemmDev& p, const ScaleDev& q, int splits, hipStream_t s) {
+  return p.c_f32 ? launch_fp8_one<C, MmaE4M3Wide>(p, q, splits, s) : launch_fp8_one<C, MmaE4M3>(p, q, splits, s);
+}
 
-typedef DmaCfg<1, 1, 2, 2, 1, 64, 3, 3, true> F8_64x64;      // TI TJ WGM WGN KW BK S OCC AHEAD
+typedef DmaCfg<1, 1, 2, 2, 1, 64, 4, 2, true> F8_64x64;      // TI TJ WGM WGN KW BK S OCC AHEAD
 typedef DmaCfg<2, 2, 2, 2, 1, 64, 2, 2, true> F8_128x128;
+typedef DmaCfg<4, 2, 2, 4, 1, 64, 2, 1, true> F8_256x256;
+
+// Sum of a split contraction's parts in their order, bias, beta; four columns per thread.  Memory bound.
+__global__ __launch_bounds__(256) void fp8_reduce_kernel(GemmDev p, int splits) {
+  const int64_t per_row = (p.N + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= per_row * p.M) return;
+  const int row = (int)(id / per_row), col = (int)(id % per_row) * 4;
+  const int have = min(4, p.N - col);
+  const float* src = p.partial + (int64_t)row * p.N + col;
+  const int64_t stride = (int64_t)p.M * p.N;
+  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if ((p.N & 3) == 0) {
+    for (int s = 0; s < splits; ++s) {
+      const float4 x = *(const float4*)(src + s * stride);
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+    }
+  } else {
+    for (int s = 0; s < splits; ++s)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (k < have) v[k] += src[s * stride + k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (k >= have) break;
+    const int64_t o = (int64_t)row * p.ldc + col + k;
+    const float x = v[k] + (p.bias ? (float)((const bf16*)p.bias)[col + k] : 0.0f);
+    if (p.c_f32) { float* C = (float*)p.C + o; *C = p.beta != 0.0f ? p.beta * *C + x : x; }
+    else ((bf16*)p.C)[o] = (bf16)x;
+  }
+}
+
+// The time of a product with each tile, in us: rounds of the chip times (w per k-tile + e), with blocks that have a CU to themselves w1 per k-tile; fitted to 8192^3,
+// 16384 x 4096 x 1024, 16384 x 1024 x 4096, 4096^3, 2048 x 1024 x 1024 and 512 x 1024 x 1024 (bf16 results: us with 64, 128, 256 tiles 836, 522, 432; 150, 90, 80; 109, 71,
+// 61; 112, 70, 60; 6.6, 7.6, 15; 4.6, 7.1, 15) and 8192^3, 1024 x 4096 x 16384, 768 x 768 x 8192 (fp32: 1293, 926, 814; 167, 130, 257; 26, 51, 130).  A split contraction pays a second launch and its partial sums' way through memory, as in gemm.hip.
+constexpr int kCUs = 256;
+struct Fp8Cfg { int b, occ; float w, w1, e; };
+const Fp8Cfg kFp8Cfg[2][3] = {{{64, 2, 0.39f, 0.17f, 1.4f}, {128, 2, 0.95f, 0.5f, 3.2f}, {256, 1, 1.58f, 1.58f, 7.3f}},
+                              {{64, 2, 0.62f, 0.36f, 2.0f}, {128, 2, 1.75f, 0.85f, 5.0f}, {256, 1, 3.2f, 3.2f, 10.0f}}};
+
+void choose_fp8(int M, int N, int K, int c_f32, size_t scratch_bytes, int* cfg, int* splits) {
+  const int kb = (K + 127) / 128;
+  float best = 3.0e38f;
+  *cfg = 0; *splits = 1;
+  for (int c = 0; c < 3; ++c) {
+    const Fp8Cfg& f = kFp8Cfg[c_f32 ? 1 : 0][c];
+    const int64_t tiles = (int64_t)((M + f.b - 1) / f.b) * ((N + f.b - 1) / f.b);
+    for (int sp = 1; sp <= 32; sp *= 2) {
+      const int steps = ((kb + sp - 1) / sp + 3) / 4 * 4;      // whole scale words
+      if (sp > 1 && (steps * (sp - 1) >= kb || (double)sp * M * N * sizeof(float) > (double)scratch_bytes)) break;
+      const int64_t n = tiles * sp, slots = (int64_t)f.occ * kCUs, rest = n % slots;
+      const float nk = (float)std::min(kb, steps);
+      float t = (float)(n / slots) * (f.w * nk + f.e) + (rest == 0 ? 0.0f : (rest <= kCUs ? f.w1 : f.w) * nk + f.e);
+      if (sp > 1) t += 3.0f + 8e-6f * sp * (float)M * (float)N / 3.5f;
+      if (t < best) { best = t; *cfg = c; *splits = sp; }
+    }
+  }
+}
 
 }  // namespace
 
@@ -301,19 +383,27 @@ hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t
   const int64_t kb = (K + (int64_t)127) / 128, most = (int64_t)1 << 22;
   if (lda % 128 || ldb % 128 || lda < 128 * kb || ldb < 128 * kb || lda > most || ldb > most || ((uintptr_t)A & 15) || ((uintptr_t)B & 15))
     return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: codes need rows of whole blocks of 128 (at most 4 MiB) and 16-byte alignment");
-  if (ldas % 4 || ldbs % 4 || ldas < kb || ldbs < kb || ((uintptr_t)as & 3) || ((uintptr_t)bs & 3))
+  if (ldas % 4 || ldbs % 4 || ldas < kb || ldbs < kb || ldas > most || ldbs > most || ((uintptr_t)as & 3) || ((uintptr_t)bs & 3))
     return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: scales need a byte per block, in rows of whole aligned 4-byte words");
   if (((uintptr_t)C % (c_f32 ? 4 : 2)) || ((uintptr_t)bias & 1)) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: C or bias is not aligned");
-  (void)scratch; (void)scratch_bytes;
+  if ((uintptr_t)scratch & 15) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: scratch must be 16-byte aligned");
   GemmDev p{};
   p.A = A; p.B = B; p.C = C; p.bias = bias;
   p.lda = lda; p.ldb = ldb; p.ldc = ldc;
   p.M = M; p.N = N; p.K = K; p.c_f32 = c_f32 ? 1 : 0; p.beta = beta;
-  p.k_per_split = std::max<int>(1, (int)(kb + 3) / 4) * 512;
+  if (((M + (int64_t)63) / 64) * ((N + (int64_t)63) / 64) * 32 > INT32_MAX) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: too many tiles");
+  int cfg, splits;
+  choose_fp8(M, N, K, p.c_f32, scratch ? scratch_bytes : 0, &cfg, &splits);
+  p.k_per_split = std::max<int>(1, (int)((kb + splits - 1) / splits + 3) / 4) * 512;
+  splits = std::max(1, (K + p.k_per_split - 1) / p.k_per_split);
+  p.partial = splits > 1 ? (float*)scratch : nullptr;
   const ScaleDev q{as, bs, ldas, ldbs};
-  if (((M + (int64_t)63) / 64) * ((N + (int64_t)63) / 64) > INT32_MAX) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: too many tiles");
-  const int64_t mid = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
-  hipError_t e = mid >= 192 ? launch_fp8<F8_128x128>(p, q, 1, (hipStream_t)stream) : launch_fp8<F8_64x64>(p, q, 1, (hipStream_t)stream);
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t e = cfg == 2 ? launch_fp8<F8_256x256>(p, q, splits, s) : cfg == 1 ? launch_fp8<F8_128x128>(p, q, splits, s) : launch_fp8<F8_64x64>(p, q, splits, s);
+  if (e == hipSuccess && splits > 1) {
+    hipLaunchKernelGGL(fp8_reduce_kernel, dim3((unsigned)(((int64_t)M * ((N + 3) / 4) + 255) / 256)), dim3(256), 0, s, p, splits);
+    e = hipGetLastError();
+  }
   return e == hipSuccess ? HS_OK : hs_fail(nullptr, HS_ERR_HIP, std::string("hs_op_gemm_fp8: ") + hipGetErrorString(e));
 }
 
