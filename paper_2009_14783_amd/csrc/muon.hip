@@ -31,9 +31,13 @@ constexpr float kSx = 256.0f;         // X is held times this
 enum { BUF_A = 0, BUF_S, BUF_T, BUF_Q, BUF_Q2, BUFS };
 __host__ __device__ constexpr float buf_scale(int b) { return b == BUF_A || b == BUF_T ? 4096.0f : b == BUF_S ? 1024.0f : 64.0f; }
 
+// The ways of a matrix: products with X in every step; polynomials of A, X in every third (see kGramAlone); a launch per step for small ones (see
+// ns_panel).
+enum NsKind { NS_BY_STEP = 0, NS_BY_GRAM, NS_BY_PANEL };
 // Matrices of one shape; `first` is the place of the first one in the table of offsets.
 struct NsGroup {
   int rows, cols, m, n, tall, count, first, parts, bufs;
+  int kind;                // NsKind: the way it goes
   int64_t ws, stride;      // bytes: first matrix' part of the workspace, and from one matrix to the next
 };
 // What a launch does to the matrices of a group.  Symmetric products: out = ident I + alpha P + beta P Q.
@@ -57,7 +61,10 @@ __device__ __forceinline__ f16* buf_ptr(char* base, const NsGroup& g, int split,
 __device__ __forceinline__ float* diag_ptr(char* base, const NsGroup& g, int split, int b) {
   return (float*)(base + 2 * x_bytes(g) + g.bufs * buf_bytes(g, split)) + (int64_t)b * g.m;
 }
+constexpr int kPanel = 64;            // columns of X that a block of the panel kernel works on
+__host__ __device__ inline size_t gram_floats(const NsGroup& g) { return (size_t)(g.n / kPanel) * g.m * g.m; }      // a step's partial A
 size_t matrix_bytes(const NsGroup& g, int split) {
+  if (g.kind == NS_BY_PANEL) return align_up(x_bytes(g) + 2 * gram_floats(g) * sizeof(float), 256);
   return align_up(2 * x_bytes(g) + g.bufs * (buf_bytes(g, split) + (size_t)g.m * sizeof(float)), 256);
 }
 
@@ -103,6 +110,49 @@ __device__ __forceinline__ float4 plain4(const PlainIO& io, int64_t i, int have,
   return make_float4(have > 0 ? (float)p[i] : 0.0f, have > 1 ? (float)p[i + 1] : 0.0f, have > 2 ? (float)p[i + 2] : 0.0f, have > 3 ? (float)p[i + 3] : 0.0f);
 }
 __device__ __forceinline__ float axpy1(const MuonIO& io, float m, float g) { return io.nesterov ? g + io.mu * m : m; }
+
+// what is orthogonalised, once the momentum is updated
+__device__ __forceinline__ float4 source4(const MuonIO& io, int64_t i, int have, bool quads) {
+  const bool whole = quads && have >= 4;
+  const float4 m = load4(io.m, i, have, whole);
+  if (!io.nesterov) return m;
+  const float4 g = gradient4(io, i, have, whole);
+  return make_float4(axpy1(io, m.x, g.x), axpy1(io, m.y, g.y), axpy1(io, m.z, g.z), axpy1(io, m.w, g.w));
+}
+__device__ __forceinline__ float4 source4(const PlainIO& io, int64_t i, int have, bool quads) { return plain4(io, i, have, quads && have >= 4); }
+
+// lr s of the update
+__device__ __forceinline__ float update_scale(const MuonIO& io, const NsGroup& g) {
+  return io.lr * (io.rms > 0.0f ? io.rms * sqrtf((float)max(g.rows, g.cols)) : sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)));
+}
+__device__ __forceinline__ float update_scale(const PlainIO&, const NsGroup&) { return 0.0f; }
+__device__ __forceinline__ void emit1(const MuonIO& io, int64_t i, float step, float y) {
+  const float w = io.decay * io.w[i] - step * y;
+  io.w[i] = w;
+  if (io.wl) io.wl[i] = (bf16)w;
+}
+__device__ __forceinline__ void emit1(const PlainIO& io, int64_t i, float, float y) { if (io.bf) ((bf16*)io.y)[i] = (bf16)y; else ((float*)io.y)[i] = y; }
+// four neighbours, `have` of which exist
+__device__ __forceinline__ void emit4(const MuonIO& io, int64_t i, int have, bool quads, float step, const float (&y)[4]) {
+  if (quads && have >= 4) {
+    float4 w = *(const float4*)(io.w + i);
+    w.x = io.decay * w.x - step * y[0]; w.y = io.decay * w.y - step * y[1]; w.z = io.decay * w.z - step * y[2]; w.w = io.decay * w.w - step * y[3];
+    *(float4*)(io.w + i) = w;
+    if (io.wl) *(bf16x4*)(io.wl + i) = bf16x4{(bf16)w.x, (bf16)w.y, (bf16)w.z, (bf16)w.w};
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) if (k < have) emit1(io, i + k, step, y[k]);
+  }
+}
+__device__ __forceinline__ void emit4(const PlainIO& io, int64_t i, int have, bool quads, float, const float (&y)[4]) {
+  if (quads && have >= 4) {
+    if (io.bf) *(bf16x4*)((bf16*)io.y + i) = bf16x4{(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+    else *(float4*)((float*)io.y + i) = make_float4(y[0], y[1], y[2], y[3]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) if (k < have) emit1(io, i + k, 0.0f, y[k]);
+  }
+}
 
 // First pass: the momentum is updated, and the sum of squares of what is going to be orthogonalised is formed in 64 bits (gradients of 1e-25 have squares
 // that 32 bits do not hold), a part of a matrix per block, added in a fixed order.  Memory bound: 12 bytes per element.
@@ -168,17 +218,7 @@ __global__ __launch_bounds__(256) void ns_start_kernel(NsDev d, IO io, double ep
   for (int k = 0; k < 4; ++k) {
     const int r = r0 + k * 16 + (threadIdx.x >> 4), have = r < g.rows ? g.cols - c0 : 0;
     const int64_t i = at.offset + r * at.ld + c0;
-    const bool whole = quads && have >= 4;
-    if constexpr (std::is_same<IO, MuonIO>::value) {
-      const float4 m = load4(io.m, i, have, whole);
-      u[k] = m;
-      if (io.nesterov) {
-        const float4 gr = gradient4(io, i, have, whole);
-        u[k] = make_float4(axpy1(io, m.x, gr.x), axpy1(io, m.y, gr.y), axpy1(io, m.z, gr.z), axpy1(io, m.w, gr.w));
-      }
-    } else {
-      u[k] = plain4(io, i, have, whole);
-    }
+    u[k] = source4(io, i, have, quads);
   }
   if (threadIdx.x < 64) {
     double s = 0.0;
@@ -317,8 +357,7 @@ void ns_product_kernel(NsDev d, IO io) {
   const NsPlace at = OP == NS_LAST ? d.table[g.first + mat] : NsPlace{0, 0};
   const bool quads = ((at.offset | at.ld) & 3) == 0;                // rows of the flat buffers start on 16 bytes
   float step = 0.0f;
-  if constexpr (UPDATE)
-    step = io.lr * (io.rms > 0.0f ? io.rms * sqrtf((float)max(g.rows, g.cols)) : sqrtf(fmaxf(1.0f, (float)g.rows / (float)g.cols)));
+  if constexpr (UPDATE) step = update_scale(io, g);
 
   // 8 neighbours of a row of the flat buffers, `have` of which exist; w: their weights, loaded before
   auto load_w = [&](int64_t i, bool whole, float (&w)[8]) __attribute__((always_inline)) {
@@ -345,36 +384,12 @@ void ns_product_kernel(NsDev d, IO io) {
         }
       } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < have) {
-            const float x = io.decay * io.w[i + k] - step * y[k];
-            io.w[i + k] = x;
-            if (io.wl) io.wl[i + k] = (bf16)x;
-          }
+        for (int k = 0; k < 8; ++k) if (k < have) emit1(io, i + k, step, y[k]);
       }
     } else if constexpr (OP == NS_LAST) {
-      if (io.bf) {
-        bf16* const o = (bf16*)io.y + i;
-        if (whole) {
-          bf16x4 a, b;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) { a[k] = (bf16)y[k]; b[k] = (bf16)y[k + 4]; }
-          *(bf16x4*)o = a;
-          *(bf16x4*)(o + 4) = b;
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) if (k < have) o[k] = (bf16)y[k];
-        }
-      } else {
-        float* const o = (float*)io.y + i;
-        if (whole) {
-          *(float4*)o = make_float4(y[0], y[1], y[2], y[3]);
-          *(float4*)(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) if (k < have) o[k] = y[k];
-        }
-      }
+      const float a[4] = {y[0], y[1], y[2], y[3]}, b[4] = {y[4], y[5], y[6], y[7]};
+      emit4(io, i, have, whole, 0.0f, a);
+      emit4(io, i + 4, have - 4, whole, 0.0f, b);
     }
   };
 
@@ -575,6 +590,271 @@ void ns_product_kernel(NsDev d, IO io) {
   if (inside) flow(std::true_type{}); else flow(std::false_type{});
 }
 
+// ---- small matrices ---------------------------------------------------------------------------------
+// With up to 128 rows all of A and S fits the LDS of a CU, and S takes it less time than a launch: every block forms S for itself and applies it to 64 columns
+// of X, which it then multiplies with themselves for its part of the next A.  One launch per step instead of three, rows padded to multiples of 32; the
+// blocks of a matrix add up each other's parts of A in their order.  What bounds it is latency, about 6 us a step with 64 rows and 11 with 128: one block of 512 threads
+// per CU.  Which lists go this way: ns_small.
+enum { PANEL_FIRST = 0, PANEL_STEP, PANEL_LAST };
+constexpr int kPanelThreads = 512, kPanelM = 128;
+constexpr int kLdS = kPanelM + 8, kLdX = kPanel + 8;      // of S and X in LDS, in fp16 numbers
+template <bool SPLIT>
+constexpr size_t panel_lds() { return (size_t)(SPLIT ? 2 : 1) * kPanelM * kLdS * 2 + 2 * (size_t)kPanelM * kLdX * 2 + 2 * kPanelM * sizeof(float); }
+
+// 32 x 32 of the sum over k < K of P[row, k] Q[k, column]: P at its row, k contiguous; Q at its column, k contiguous (KMAJ) or columns contiguous
+template <bool SPLIT, bool KMAJ, int K>
+__device__ __forceinline__ void panel_product(f32x16& acc, const f16* p, int ldp, int lop, const f16* q, int ldq, int loq, int lane) {
+  typedef s16x4 __attribute__((address_space(3))) * lds_v4;
+  const int h = lane >> 5;
+  auto rows = [&](const f16* b, int ld, int k) __attribute__((always_inline)) { return *(const f16x8*)(b + (lane & 31) * ld + k + 8 * h); };
+  auto cols = [&](const f16* b, int ld, int k) __attribute__((always_inline)) {      // the transposing read of DmaTile::frag
+    const f16* const at = b + (k + 8 * h + ((lane & 15) >> 2)) * ld + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    union { struct { s16x4 lo, hi; } v; f16x8 f; } u;
+    u.v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4)at);
+    u.v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4)(at + 4 * ld));
+    return u.f;
+  };
+#pragma unroll
+  for (int k = 0; k < K; k += 16) {
+    const f16x8 ph = rows(p, ldp, k), qh = KMAJ ? rows(q, ldq, k) : cols(q, ldq, k);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+    if (SPLIT) {
+      const f16x8 pl = rows(p + lop, ldp, k), ql = KMAJ ? rows(q + loq, ldq, k) : cols(q + loq, ldq, k);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
+    }
+  }
+}
+
+template <bool SPLIT, int MODE, int M, class IO>
+__device__ __forceinline__ void ns_panel(const NsDev& d, const IO& io, double eps, const NsJob& job, int local, unsigned char* lds_raw, double* inv_s) {
+  constexpr int kLoS = kPanelM * kLdS, kLoX = kPanelM * kLdX;      // second numbers
+  f16* const sS = (f16*)lds_raw;                                   // E of A, then of S
+  f16* const sX = sS + (SPLIT ? 2 : 1) * kLoS;
+  float* const sD = (float*)(sX + 2 * kLoX);                       // diagonal of A; of S behind it
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const NsGroup& g = job.g;
+  constexpr int m = M, mt = M / 32, TILES = mt * mt, TPW = (TILES + 7) / 8;      // 32 x 32 tiles of a square matrix, and per wave
+  const int n = g.n, panels = n / kPanel, mat = local / panels, j0 = local % panels * kPanel;
+  char* const base = d.ws + g.ws + mat * g.stride;
+  f16* const X = (f16*)base;
+  const int64_t lo_at = (int64_t)m * n;
+  float* const gram = (float*)(base + x_bytes(g));
+  const float* const old = gram + d.from * gram_floats(g);
+  float* const now = gram + (d.from ^ 1) * gram_floats(g) + (int64_t)(j0 / kPanel) * m * m;
+  const NsPlace at = MODE == PANEL_STEP ? NsPlace{0, 0} : d.table[g.first + mat];
+  const bool quads = ((at.offset | at.ld) & 3) == 0;
+  // rows and columns of a result tile that a lane holds: 4 rows from row(r) on in register 4 r .. 4 r + 3, one column
+  auto row = [&](int r) __attribute__((always_inline)) { return 8 * r + 4 * (lane >> 5); };
+  const int col = lane & 31;
+
+  if constexpr (MODE == PANEL_FIRST) {
+    if (tid < 64) {
+      double s = 0.0;
+      for (int k = tid; k < g.parts; k += 64) s += d.partial[(int64_t)(g.first + mat) * kParts + k];
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+      if (tid == 0) *inv_s = s == 0.0 ? 0.0 : (double)kSx / (sqrt(s) + eps);      // a matrix of zeros stays one
+    }
+    // four neighbours of a row of the matrix: of X's row, or of its column where the matrix is tall
+    const int per_row = (g.tall ? m : kPanel) / 4, total = m * kPanel / 4;
+    float4 u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = tid + k * kPanelThreads, lr = e / per_row, lc = (e % per_row) * 4;
+      const int r = g.tall ? j0 + lr : lr, c = g.tall ? lc : j0 + lc;
+      u[k] = source4(io, at.offset + (int64_t)r * at.ld + c, e < total && r < g.rows ? g.cols - c : 0, quads);
+    }
+    __syncthreads();
+    const double inv = *inv_s;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = tid + k * kPanelThreads, lr = e / per_row, lc = (e % per_row) * 4;
+      if (e >= total) break;
+      const float x[4] = {(float)((double)u[k].x * inv), (float)((double)u[k].y * inv), (float)((double)u[k].z * inv), (float)((double)u[k].w * inv)};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        f16* const o = g.tall ? sX + (lc + c) * kLdX + lr : sX + lr * kLdX + lc + c;
+        const f16 h = (f16)x[c];
+        o[0] = h; o[kLoX] = (f16)(x[c] - (float)h);
+      }
+    }
+  } else {
+    // X of the panel, and A: the sum of the blocks' parts
+    for (int e = tid; e < m * kPanel / 8; e += kPanelThreads) {
+      const int r = e / (kPanel / 8), c = (e % (kPanel / 8)) * 8;
+      const f16* const src = X + (int64_t)r * n + j0 + c;
+      *(f16x8*)(sX + r * kLdX + c) = *(const f16x8*)src;
+      *(f16x8*)(sX + kLoX + r * kLdX + c) = *(const f16x8*)(src + lo_at);
+    }
+    // (several parts in flight at once: read one after the other they cost 2 us each)
+    constexpr int QUADS = M * M / 4, NQ = (QUADS + kPanelThreads - 1) / kPanelThreads, AHEAD = 32 / NQ > 8 ? 8 : 32 / NQ;      // of a thread; parts in flight
+    float4 a[NQ];
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4* const src = (const float4*)old;
+    for (int p = 0; p < panels; p += AHEAD) {
+      float4 v[AHEAD][NQ];
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) v[q][k] = src[(int64_t)min(p + q, panels - 1) * QUADS + min(tid + k * kPanelThreads, QUADS - 1)];
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q)
+        if (p + q < panels) {
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) { a[k].x += v[q][k].x; a[k].y += v[q][k].y; a[k].z += v[q][k].z; a[k].w += v[q][k].w; }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) {
+      const int e = tid + k * kPanelThreads, r = e / (M / 4), c = (e % (M / 4)) * 4;
+      if (e >= QUADS) break;
+      const float x[4] = {a[k].x, a[k].y, a[k].z, a[k].w};
+      f16x4 h, l;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (r == c + t) sD[r] = x[t] * (1.0f / buf_scale(BUF_A));
+        const float v = r == c + t ? 0.0f : x[t];
+        h[t] = (f16)v; l[t] = (f16)(v - (float)h[t]);
+      }
+      *(f16x4*)(sS + r * kLdS + c) = h;
+      if (SPLIT) *(f16x4*)(sS + kLoS + r * kLdS + c) = l;
+    }
+    __syncthreads();
+
+    // S = a I + b A + c A A with the diagonals apart, as in ns_product_kernel; up to two tiles per wave
+    f32x16 s[TPW];
+    float sd[TPW];      // a diagonal element that this lane has
+#pragma unroll
+    for (int q = 0; q < TPW; ++q) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[q][r] = 0.0f;
+      const int id = wave + 8 * q;
+      if (id >= TILES) continue;
+      const int ti = id / mt * 32, tj = id % mt * 32;
+      panel_product<SPLIT, true, M>(s[q], sS + ti * kLdS, kLdS, kLoS, sS + tj * kLdS, kLdS, kLoS, lane);
+      const float dc = sD[tj + col];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {      // A is symmetric: four elements of a column are read as four of a row
+        const int i0 = ti + row(r), j = tj + col;
+        const f16x4 eh = *(const f16x4*)(sS + j * kLdS + i0);
+        f16x4 el = {};
+        if (SPLIT) el = *(const f16x4*)(sS + kLoS + j * kLdS + i0);
+        const float4 d4 = *(const float4*)(sD + i0);
+        const float dr[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float e = ((float)eh[t] + (float)el[t]) * (1.0f / buf_scale(BUF_A)), prod = s[q][4 * r + t] * (1.0f / (buf_scale(BUF_A) * buf_scale(BUF_A)));
+          if (i0 + t == j) { sd[q] = job.ident + job.alpha * dr[t] + job.beta * (prod + dr[t] * dr[t]); s[q][4 * r + t] = 0.0f; }
+          else s[q][4 * r + t] = (job.alpha * e + job.beta * (prod + (dr[t] + dc) * e)) * buf_scale(BUF_S);
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < TPW; ++q) {
+      const int id = wave + 8 * q;
+      if (id >= TILES) continue;
+      const int ti = id / mt * 32, tj = id % mt * 32;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {      // symmetric: written as column tj + col's four neighbours
+        f16x4 h, l;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float v = s[q][4 * r + t];
+          h[t] = (f16)v; l[t] = (f16)(v - (float)h[t]);
+          if (ti + row(r) + t == tj + col) sD[kPanelM + tj + col] = sd[q];
+        }
+        f16* const o = sS + (tj + col) * kLdS + ti + row(r);
+        *(f16x4*)o = h;
+        if (SPLIT) *(f16x4*)(o + kLoS) = l;
+      }
+    }
+    __syncthreads();
+
+    // X <- (D + E) X; a tile per wave
+    f32x16 x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+    const int ti = wave / 2 * 32, tj = wave % 2 * 32;
+    if (ti < m) {
+      panel_product<SPLIT, false, M>(x, sS + ti * kLdS, kLdS, kLoS, sX + tj, kLdX, kLoX, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = ti + row(r >> 2) + (r & 3);
+        const f16* const o = sX + i * kLdX + tj + col;
+        x[r] = sD[kPanelM + i] * ((float)o[0] + (float)o[kLoX]) + x[r] * (1.0f / buf_scale(BUF_S));
+      }
+    }
+    if constexpr (MODE == PANEL_LAST) {
+      if (ti < m) {
+        const float step = update_scale(io, g);
+        const int j = j0 + tj + col;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = ti + row(r);
+          const float y[4] = {x[4 * r] * (1.0f / kSx), x[4 * r + 1] * (1.0f / kSx), x[4 * r + 2] * (1.0f / kSx), x[4 * r + 3] * (1.0f / kSx)};
+          if (g.tall) {
+            if (j < g.rows) emit4(io, at.offset + (int64_t)j * at.ld + i, g.cols - i, quads, step, y);
+          } else if (j < g.cols) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) if (i + t < g.rows) emit1(io, at.offset + (int64_t)(i + t) * at.ld + j, step, y[t]);
+          }
+        }
+      }
+      return;
+    }
+    __syncthreads();
+    if (ti < m) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        f16* const o = sX + (ti + row(r >> 2) + (r & 3)) * kLdX + tj + col;
+        const f16 h = (f16)x[r];
+        o[0] = h; o[kLoX] = (f16)(x[r] - (float)h);
+      }
+    }
+  }
+  if constexpr (MODE != PANEL_LAST) {
+    __syncthreads();
+    for (int e = tid; e < m * kPanel / 8; e += kPanelThreads) {
+      const int r = e / (kPanel / 8), c = (e % (kPanel / 8)) * 8;
+      f16* const o = X + (int64_t)r * n + j0 + c;
+      *(f16x8*)o = *(const f16x8*)(sX + r * kLdX + c);
+      *(f16x8*)(o + lo_at) = *(const f16x8*)(sX + kLoX + r * kLdX + c);
+    }
+    // this panel's part of the next A
+#pragma unroll
+    for (int q = 0; q < TPW; ++q) {
+      const int id = wave + 8 * q;
+      if (id >= TILES) continue;
+      const int ti = id / mt * 32, tj = id % mt * 32;
+      f32x16 s;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+      panel_product<SPLIT, true, kPanel>(s, sX + ti * kLdX, kLdX, kLoX, sX + tj * kLdX, kLdX, kLoX, lane);
+      constexpr float f = buf_scale(BUF_A) / (kSx * kSx);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(float4*)(now + (int64_t)(tj + col) * m + ti + row(r)) = make_float4(s[4 * r] * f, s[4 * r + 1] * f, s[4 * r + 2] * f, s[4 * r + 3] * f);
+    }
+  }
+}
+
+template <bool SPLIT, int MODE, class IO>
+__global__ __launch_bounds__(kPanelThreads) void ns_panel_kernel(NsDev d, IO io, double eps) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
+  __shared__ double inv_s;
+  const int ji = ns_job(d, blockIdx.x), local = blockIdx.x - d.first_block[ji];
+  const NsJob& job = d.job[ji];
+  switch (job.g.m) {
+    case 32: ns_panel<SPLIT, MODE, 32>(d, io, eps, job, local, lds_raw, &inv_s); break;
+    case 64: ns_panel<SPLIT, MODE, 64>(d, io, eps, job, local, lds_raw, &inv_s); break;
+    case 96: ns_panel<SPLIT, MODE, 96>(d, io, eps, job, local, lds_raw, &inv_s); break;
+    default: ns_panel<SPLIT, MODE, 128>(d, io, eps, job, local, lds_raw, &inv_s); break;
+  }
+}
+
 typedef DmaCfg<1, 1, 1, 1, 4, 64, 4, 1, false> Ns32;      // TI TJ WGM WGN KW BK S OCC AHEAD
 typedef DmaCfg<1, 1, 2, 2, 1, 64, 3, 3, true> Ns64;
 typedef DmaCfg<2, 2, 2, 2, 1, 64, 2, 2, true> Ns128;
@@ -586,7 +866,7 @@ int64_t ns_tiles(const NsGroup& g, int op, int bm, int bn) {
 }
 
 constexpr int kCUs = 256;
-struct NoIO {};
+struct NoIO {};      // products that stay in the workspace
 template <class C, int OP, bool SPLIT, class IO>
 hipError_t launch_product(NsDev& d, const IO& io, hipStream_t s) {
   int64_t blocks = 0;
@@ -631,6 +911,23 @@ hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
 // stack of layers with square matrices from 8e10 on (12 layers of hidden 512: 1037, 1082; 3 of 768: 723, 699; 24 of 1024: 8.6 ms, 10.1 ms).
 constexpr double kGramAlone = 1.5e10, kGramBeside = 8e10;
 
+// Whether a list goes through the panel kernel: up to 128 rows in every matrix, blocks for about one round of the chip, and not too much to read of each other's
+// parts of A (a matrix of P panels: P P m m floats in a step).  Whole list in us, with and without: 130 x 67 in 32 bits 72, 107; 64 x 64 42, 94; 16 of
+// 64 x 1024 (64 MB) 77, 106, 64 of them 223, 142; 24 layers of hidden 64 (288 blocks) 89, 107, 48 of them 132, 122; of 128 rows, whose steps are longer: toy model
+// 113, 121 (9 MB); 16 of 128 x 256 (17 MB) 94, 99; 16 of 128 x 512 (67 MB) 127, 103.
+bool ns_small(const std::vector<NsGroup>& groups) {
+  int64_t blocks = 0, bytes = 0;
+  int rows = 0;
+  for (const NsGroup& g : groups) {
+    const int64_t m = (std::min(g.rows, g.cols) + 31) / 32 * 32, panels = g.n / kPanel;
+    if (m > kPanelM) return false;
+    rows = std::max(rows, (int)m);
+    blocks += g.count * panels;
+    bytes += g.count * panels * panels * m * m * 4;
+  }
+  return blocks <= 288 && bytes <= (rows > 96 ? (int64_t)17 << 20 : (int64_t)72 << 20);
+}
+
 // The shapes of a list and the order of its matrices, shape by shape; the workspace is laid out as [table][partial sums][matrices].
 struct NsPlan {
   std::vector<NsGroup> groups;
@@ -661,6 +958,7 @@ NsPlan ns_plan(const hs_matrix* mats, int n, int split) {
     p.groups.push_back(g);
     i = j;
   }
+  const bool small = ns_small(p.groups);
   double saved = 0.0;
   bool others = false;
   for (const NsGroup& g : p.groups) {
@@ -669,7 +967,9 @@ NsPlan ns_plan(const hs_matrix* mats, int n, int split) {
   }
   const bool gram = saved >= (others ? kGramBeside : kGramAlone);
   for (NsGroup& g : p.groups) {
-    g.bufs = gram && g.n >= 2 * g.m ? BUFS : BUF_S + 1;
+    g.kind = small ? NS_BY_PANEL : gram && g.n >= 2 * g.m ? NS_BY_GRAM : NS_BY_STEP;
+    if (small) g.m = (std::min(g.rows, g.cols) + 31) / 32 * 32;
+    g.bufs = g.kind == NS_BY_GRAM ? BUFS : BUF_S + 1;
     g.ws = (int64_t)off; g.stride = (int64_t)matrix_bytes(g, split);
     off += (size_t)g.stride * g.count;
   }
@@ -710,9 +1010,23 @@ bool ns_disjoint(const hs_matrix* mats, int n) {
   return true;
 }
 
-// The whole of it for groups that go through the same products.
+template <bool SPLIT, int MODE, class IO>
+hipError_t launch_panel(const NsDev& d, const IO& io, double eps, unsigned blocks, hipStream_t s) {
+  auto kern = ns_panel_kernel<SPLIT, MODE, IO>;
+  constexpr size_t lds = panel_lds<SPLIT>();
+  static bool configured = false;      // per instantiation, as in gemm_wide.h
+  if (!configured) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  configured = true;
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(kPanelThreads), lds, s, d, io, eps);
+  return hipGetLastError();
+}
+
+// The whole of it for groups that go the same way.
 template <class IO>
-hipError_t ns_run(const std::vector<NsGroup>& groups, bool gram, int split, char* ws, const NsPlace* table, double* partial, const IO& io, int steps,
+hipError_t ns_run(const std::vector<NsGroup>& groups, int kind, int split, char* ws, const NsPlace* table, double* partial, const IO& io, int steps,
                   const double* c, double eps, hipStream_t s) {
   NsDev d{};
   d.split = split; d.ws = ws; d.table = table; d.partial = partial;
@@ -728,6 +1042,18 @@ hipError_t ns_run(const std::vector<NsGroup>& groups, bool gram, int split, char
   add(0, 0, 0, 0.0, 0.0, 0.0);
   unsigned blocks = blocks_of([](const NsGroup& g) { return g.parts; });
   hipLaunchKernelGGL(ns_norm_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io);
+  if (kind == NS_BY_PANEL) {
+    blocks = blocks_of([](const NsGroup& g) { return g.n / kPanel; });
+    hipError_t e = split ? launch_panel<true, PANEL_FIRST>(d, io, eps, blocks, s) : launch_panel<false, PANEL_FIRST>(d, io, eps, blocks, s);
+    for (int k = 0; k < steps && e == hipSuccess; ++k) {
+      d.from ^= 1;
+      for (int i = 0; i < d.n; ++i) { d.job[i].ident = (float)c[3 * k]; d.job[i].alpha = (float)c[3 * k + 1]; d.job[i].beta = (float)c[3 * k + 2]; }
+      if (k + 1 < steps) e = split ? launch_panel<true, PANEL_STEP>(d, io, eps, blocks, s) : launch_panel<false, PANEL_STEP>(d, io, eps, blocks, s);
+      else e = split ? launch_panel<true, PANEL_LAST>(d, io, eps, blocks, s) : launch_panel<false, PANEL_LAST>(d, io, eps, blocks, s);
+    }
+    return e;
+  }
+  const bool gram = kind == NS_BY_GRAM;
   blocks = blocks_of([](const NsGroup& g) { return (g.m / 64) * (g.n / 64); });
   hipLaunchKernelGGL(ns_start_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io, eps);
   hipError_t e = hipGetLastError();
@@ -809,12 +1135,17 @@ hs_status orthogonalize(const char* who, const IO& io, size_t size, const hs_mat
   }
   std::vector<double> c(3 * steps);
   for (int k = 0; k < 3 * steps; ++k) c[k] = coeff ? coeff[k] : kDefaultCoeff[k % 3];
-  // runs of groups that go through the same products, as many as the jobs of a launch
-  for (size_t g0 = 0; g0 < plan.groups.size() && e == hipSuccess;) {
+  // runs of groups that go the same way, as many as the jobs of a launch
+  for (int kind : {NS_BY_STEP, NS_BY_GRAM, NS_BY_PANEL}) {
     std::vector<NsGroup> now;
-    const bool gram = plan.groups[g0].bufs == BUFS;
-    for (; g0 < plan.groups.size() && now.size() < kJobs / 2 && (plan.groups[g0].bufs == BUFS) == gram; ++g0) now.push_back(plan.groups[g0]);
-    e = ns_run(now, gram, split, ws, table, (double*)(ws + plan.partial), io, steps, c.data(), eps, s);
+    const size_t most = kind == NS_BY_GRAM ? kJobs / 2 : kJobs;      // two products of a group in one launch
+    for (size_t i = 0; i <= plan.groups.size() && e == hipSuccess; ++i) {
+      if (!now.empty() && (i == plan.groups.size() || now.size() == most)) {
+        e = ns_run(now, kind, split, ws, table, (double*)(ws + plan.partial), io, steps, c.data(), eps, s);
+        now.clear();
+      }
+      if (i < plan.groups.size() && plan.groups[i].kind == kind) now.push_back(plan.groups[i]);
+    }
   }
   return e == hipSuccess ? HS_OK : hs_fail(nullptr, HS_ERR_HIP, name + hipGetErrorString(e));
 }

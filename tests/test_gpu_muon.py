@@ -79,6 +79,35 @@ def test_list_of_odd_shapes(hs, products, dtype, gap, ld):
     assert np.all(got[rest] == 7.5)
 
 
+SMALL = {"to 96 rows": [(1, 1), (1, 7), (5, 1), (37, 53), (64, 64), (65, 64), (64, 65), (96, 300), (90, 100), (64, 1000), (1000, 33), (100, 3), (130, 67)],
+         "to 128 rows": [(128, 128), (128, 512), (127, 300), (512, 100), (1, 1), (130, 67), (30, 40)], "one long": [(64, 4000)], "one tall": [(2000, 20)],
+         "one too many": [(128, 512)] * 16}
+
+
+@pytest.mark.parametrize("products", [0, 1])
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("gap,ld", [(0, 0), (3, 0), (8, 5)])
+@pytest.mark.parametrize("which", list(SMALL))
+def test_list_of_small_shapes(hs, products, dtype, gap, ld, which):
+    """Lists without a larger matrix among them go a way of their own: up to 128 rows, one and several panels of 64 columns."""
+    shapes = SMALL[which]
+    mats, size = layout(shapes, gap, ld)
+    x = torch.from_numpy(gaussian(np.random.default_rng(10 + gap), size)).to(torch.bfloat16 if dtype else torch.float32)
+    y = torch.full_like(x, 7.5).cuda()
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, products)
+    hs.hs_op_orthogonalize(dtype, x.cuda(), y, size, lst, products, 5, None, 1e-7, ws, n)
+    torch.cuda.synchronize()
+    got, flat = y.cpu().double().numpy(), x.double().numpy()
+    for mat in mats:
+        tol, e = tolerance(view(flat, mat), products)
+        assert rel(view(got, mat), e) <= tol + (2.0 ** -8 if dtype else 0.0), mat
+    rest = np.ones(size, bool)
+    for mat in mats:
+        view(rest, mat)[...] = False
+    assert np.all(got[rest] == 7.5)
+
+
 @pytest.mark.parametrize("products", [0, 1])
 @pytest.mark.parametrize("shape,count", [((768, 768), 2), ((1024, 640), 3), ((600, 2000), 2), ((256, 256), 40)])
 def test_larger_matrices(hs, products, shape, count):
@@ -230,8 +259,9 @@ def muon_tolerances(w, m, G, lr, momentum, nesterov, weight_decay, rms, denom, p
 @pytest.mark.parametrize("products", [0, 1])
 @pytest.mark.parametrize("nesterov,denom,rms,wd,lowp", [(1, 48.0, 0.2, 0.1, True), (0, 0.0, 0.0, 0.0, False), (1, 0.0, 0.2, 0.0, True)])
 @pytest.mark.parametrize("gap,ld", [(0, 0), (5, 3)])
-def test_update_of_a_list(hs, products, nesterov, denom, rms, wd, lowp, gap, ld):
-    mats, size = layout([(1, 1), (64, 192), (192, 64), (37, 53), (300, 520), (130, 67)], gap, ld)
+@pytest.mark.parametrize("small", [False, True])
+def test_update_of_a_list(hs, products, nesterov, denom, rms, wd, lowp, gap, ld, small):
+    mats, size = layout([(1, 1), (64, 192), (192, 64), (37, 53), (130, 67)] + ([] if small else [(300, 520)]), gap, ld)
     rng = np.random.default_rng(gap + int(denom))
     w, m, G = 0.02 * gaussian(rng, size), 1e-3 * gaussian(rng, size), np.float32(max(denom, 1.0)) * 1e-3 * gaussian(rng, size)
     dw, dm, dG = (torch.from_numpy(a.copy()).cuda() for a in (w, m, G))
