@@ -287,7 +287,7 @@ hipError_t launch_fp8_one(const GemmDev& p, const ScaleDev& q, int splits, hipSt
     if (e != hipSuccess) return e;
   }
   configured = true;
-  const int nbx = (p.N + C::BN - 1) / C::BN, nby = (p.M + C::BM - 1) / C::BM;
+  const int nbx = (int)((p.N + (int64_t)C::BN - 1) / C::BN), nby = (int)((p.M + (int64_t)C::BM - 1) / C::BM);
   hipLaunchKernelGGL(kern, dim3((unsigned)(nbx * nby * splits)), dim3(C::NT), lds, s, p, q, nbx, nby);
   return hipGetLastError();
 }
@@ -343,10 +343,10 @@ void choose_fp8(int M, int N, int K, int c_f32, size_t scratch_bytes, int* cfg, 
   *cfg = 0; *splits = 1;
   for (int c = 0; c < 3; ++c) {
     const Fp8Cfg& f = kFp8Cfg[c_f32 ? 1 : 0][c];
-    const int64_t tiles = (int64_t)((M + f.b - 1) / f.b) * ((N + f.b - 1) / f.b);
+    const int64_t tiles = ((M + (int64_t)f.b - 1) / f.b) * ((N + (int64_t)f.b - 1) / f.b);
     for (int sp = 1; sp <= 32; sp *= 2) {
       const int steps = ((kb + sp - 1) / sp + 3) / 4 * 4;      // whole scale words
-      if (sp > 1 && (steps * (sp - 1) >= kb || (double)sp * M * N * sizeof(float) > (double)scratch_bytes)) break;
+      if (sp > 1 && (steps * (sp - 1) >= kb || (double)sp * M * N * sizeof(float) > (double)scratch_bytes || (double)M * N > 4e9)) break;
       const int64_t n = tiles * sp, slots = (int64_t)f.occ * kCUs, rest = n % slots;
       const float nk = (float)std::min(kb, steps);
       float t = (float)(n / slots) * (f.w * nk + f.e) + (rest == 0 ? 0.0f : (rest <= kCUs ? f.w1 : f.w) * nk + f.e);
@@ -375,7 +375,7 @@ hs_status hs_op_quantize_fp8(int32_t dtype, const void* x, int64_t ldx, int32_t 
     return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_quantize_fp8: q needs rows of whole blocks of 128 and 16-byte alignment, qs a byte per block");
   if (qt && (ldqt % 128 || ldqt < 128 * rb || ldqts < rb || ((uintptr_t)qt & 15)))
     return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_quantize_fp8: qt needs rows of whole blocks of 128 and 16-byte alignment, qts a byte per block");
-  if (cb * rb > INT32_MAX) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_quantize_fp8: too many blocks");
+  if (cb * rb >= ((int64_t)1 << 32) / kQuantThreads) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_quantize_fp8: too many blocks");      // threads of one launch
   QuantDev p{x, ldx, R, C, tile, (uint8_t*)q, qs, (uint8_t*)qt, qts, ldq, ldqs, ldqt, ldqts, (int)cb};
   hipLaunchKernelGGL(dtype == HS_BF16 ? quantize_fp8_kernel<bf16> : quantize_fp8_kernel<float>, dim3((unsigned)(cb * rb)), dim3(kQuantThreads), 0,
                      (hipStream_t)stream, p);
@@ -401,11 +401,12 @@ hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t
   p.A = A; p.B = B; p.C = C; p.bias = bias;
   p.lda = lda; p.ldb = ldb; p.ldc = ldc;
   p.M = M; p.N = N; p.K = K; p.c_f32 = c_f32 ? 1 : 0; p.beta = beta;
-  if (((M + (int64_t)63) / 64) * ((N + (int64_t)63) / 64) * 32 > INT32_MAX) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: too many tiles");
   int cfg, splits;
   choose_fp8(M, N, K, p.c_f32, scratch ? scratch_bytes : 0, &cfg, &splits);
   p.k_per_split = std::max<int>(1, (int)((kb + splits - 1) / splits + 3) / 4) * 512;
   splits = std::max(1, (K + p.k_per_split - 1) / p.k_per_split);
+  const int64_t bt = kFp8Cfg[0][cfg].b, blocks = ((M + bt - 1) / bt) * ((N + bt - 1) / bt) * splits;
+  if (blocks >= ((int64_t)1 << 32) / 512) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: too many tiles");      // threads of one launch
   p.partial = splits > 1 ? (float*)scratch : nullptr;
   const ScaleDev q{as, bs, ldas, ldbs};
   hipStream_t s = (hipStream_t)stream;

@@ -15,6 +15,7 @@
 // along: three products hi hi + hi lo + lo hi as one contraction three times as long, error as in fp32.
 #include <algorithm>
 #include <cmath>
+#include <new>
 #include <numeric>
 #include <tuple>
 
@@ -888,8 +889,9 @@ template <int OP, class IO>
 hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
   // Rounds that the tiles of a size take on the chip (one 256 x 256 tile per CU, two of 128 x 128, three of 64 x 64) times what a round takes, as a share of one
   // of 256 x 256 tiles, from lists of 48 and 96 matrices of 1024 x 1024 and 1024 x 4096 (us with 256, 128, 64: GRAM 171, 189, 219; SYM 216, 211, 242; APPLY
-  // 303, 335, 466).  256 x 256 tiles are not built for 32-bit products.
-  constexpr float kRound128 = OP == NS_SYM ? 0.48f : 0.55f, kRound64 = OP == NS_SYM ? 0.21f : OP == NS_GRAM ? 0.24f : 0.28f;
+  // 303, 335, 466).  256 x 256 tiles are not built for 32-bit products, nor taken by SYM.  A launch whose 32 x 32 tiles all have a CU takes
+  // those, whose waves split the contraction (toy model 133 -> 117 us, one matrix 256 x 2048 135 -> 113).
+  constexpr float kRound128 = OP == NS_SYM ? 0.48f : OP == NS_GRAM ? 0.60f : 0.55f, kRound64 = OP == NS_SYM ? 0.25f : 0.29f;
   auto rounds = [&](int b, int slots) {
     int64_t tiles = 0;
     for (int i = 0; i < d.n; ++i) tiles += ns_tiles(d.job[i].g, OP, b, b);
@@ -1102,7 +1104,7 @@ hipError_t ns_run(const std::vector<NsGroup>& groups, int kind, int split, char*
 const double kDefaultCoeff[3] = {3.4445, -4.7750, 2.0315};
 
 template <class IO>
-hs_status orthogonalize(const char* who, const IO& io, size_t size, const hs_matrix* mats, int32_t n, int32_t products, int32_t steps,
+hs_status orthogonalize_checked(const char* who, const IO& io, size_t size, const hs_matrix* mats, int32_t n, int32_t products, int32_t steps,
                         const double* coeff, double eps, void* workspace, size_t workspace_bytes, hipStream_t s) {
   const std::string name = std::string(who) + ": ";
   std::string why;
@@ -1150,6 +1152,17 @@ hs_status orthogonalize(const char* who, const IO& io, size_t size, const hs_mat
   return e == hipSuccess ? HS_OK : hs_fail(nullptr, HS_ERR_HIP, name + hipGetErrorString(e));
 }
 
+// no exception leaves a C entry
+template <class IO>
+hs_status orthogonalize(const char* who, const IO& io, size_t size, const hs_matrix* mats, int32_t n, int32_t products, int32_t steps,
+                        const double* coeff, double eps, void* workspace, size_t workspace_bytes, hipStream_t s) {
+  try {
+    return orthogonalize_checked(who, io, size, mats, n, products, steps, coeff, eps, workspace, workspace_bytes, s);
+  } catch (const std::bad_alloc&) {
+    return hs_fail(nullptr, HS_ERR_STATE, "out of host memory");
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -1160,7 +1173,12 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
     hs_fail(nullptr, HS_ERR_INVALID_ARG, "hs_orthogonalize_workspace_bytes: " + (why.empty() ? "products must be HS_FP32 or HS_BF16" : why));
     return 0;
   }
-  return ns_plan(mats, n, products == HS_FP32).total;
+  try {
+    return ns_plan(mats, n, products == HS_FP32).total;
+  } catch (const std::bad_alloc&) {
+    hs_fail(nullptr, HS_ERR_STATE, "hs_orthogonalize_workspace_bytes: out of host memory");
+    return 0;
+  }
 }
 
 hs_status hs_op_orthogonalize(int32_t dtype, const void* x, void* y, size_t size, const hs_matrix* mats, int32_t n, int32_t products, int32_t steps,

@@ -214,10 +214,11 @@ def test_zeros_stay_zeros_and_what_is_not_finite_stays_in_its_matrix(hs):
                 assert rel(view(got, mat), e) <= tol
 
 
-def test_many_matrices_and_more_shapes_than_one_launch_takes(hs):
-    """450 matrices of 45 shapes, in an order that mixes them."""
+@pytest.mark.parametrize("count,beside", [(280, []), (450, [(300, 300)])])
+def test_many_matrices_and_more_shapes_than_one_launch_takes(hs, count, beside):
+    """Hundreds of matrices of 45 shapes, in an order that mixes them, by themselves and beside one that is not small."""
     rng = np.random.default_rng(5)
-    shapes = [(1 + i % 9, 2 + (i * 7) % 45) for i in range(450)]
+    shapes = beside + [(1 + i % 9, 2 + (i * 7) % 45) for i in range(count)]
     mats, size = layout(shapes, 1)
     x = gaussian(rng, size)
     lst = hs.make_matrices(mats)

@@ -23,7 +23,7 @@ def quant(dtype=1, x=P, ldx=200, R=37, C=200, tile=0, q=P, ldq=256, qs=P, ldqs=4
     (dict(dtype=2), INVALID), (dict(R=-1), INVALID), (dict(C=-1), INVALID), (dict(tile=2), INVALID), (dict(x=None), INVALID), (dict(q=None), INVALID),
     (dict(qs=None), INVALID), (dict(qt=None), INVALID), (dict(q=None, qs=None, qt=None, qts=None), INVALID), (dict(ldx=199), SHAPE), (dict(ldq=200), SHAPE),
     (dict(ldq=128), SHAPE), (dict(ldqs=1), SHAPE), (dict(ldqt=64), SHAPE), (dict(ldqts=0), SHAPE), (dict(q=P + 8), SHAPE), (dict(qt=P + 8), SHAPE),
-    (dict(x=P + 1), SHAPE)])
+    (dict(x=P + 1), SHAPE), (dict(R=2 ** 31 - 1, C=2 ** 31 - 1, ldx=2 ** 31, ldq=2 ** 31, ldqs=2 ** 24, ldqt=2 ** 31, ldqts=2 ** 24), SHAPE)])
 def test_quantiser_refuses(change, status):
     refused(status, hs.hs_op_quantize_fp8, *quant(**change))
 
@@ -46,7 +46,8 @@ def gemm(M=5, N=6, K=200, A=P, lda=256, sa=P, ldas=4, B=P, ldb=256, sb=P, ldbs=4
     (dict(M=-1), INVALID), (dict(N=-1), INVALID), (dict(K=-1), INVALID), (dict(A=None), INVALID), (dict(sa=None), INVALID), (dict(B=None), INVALID),
     (dict(sb=None), INVALID), (dict(C=None), INVALID), (dict(ldc=5), SHAPE), (dict(lda=200), SHAPE), (dict(lda=128), SHAPE), (dict(ldb=128), SHAPE),
     (dict(lda=1 << 23), SHAPE), (dict(ldas=2), SHAPE), (dict(ldbs=0), SHAPE), (dict(K=600, lda=640, ldb=640, ldbs=4), SHAPE), (dict(A=P + 8), SHAPE),
-    (dict(B=P + 4), SHAPE), (dict(sa=P + 1), SHAPE), (dict(sb=P + 2), SHAPE), (dict(C=P + 2, c_f32=1), SHAPE), (dict(C=P + 1), SHAPE), (dict(bias=P + 1), SHAPE)])
+    (dict(B=P + 4), SHAPE), (dict(sa=P + 1), SHAPE), (dict(sb=P + 2), SHAPE), (dict(C=P + 2, c_f32=1), SHAPE), (dict(C=P + 1), SHAPE), (dict(bias=P + 1), SHAPE), (dict(scratch=P + 8, scratch_bytes=1 << 20), SHAPE),
+    (dict(M=2 ** 31 - 1, N=2 ** 31 - 1, ldc=2 ** 31), SHAPE), (dict(ldas=1 << 23), SHAPE)])
 def test_product_refuses(change, status):
     args, kw = gemm(**change)
     refused(status, hs.hs_op_gemm_fp8, *args, **kw)
