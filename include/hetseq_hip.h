@@ -332,8 +332,8 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
  * 0.005 to 1 times the largest into 0.7 .. 1.2).
  * dtype: element type of x and y (flat buffers of `size` elements, in which the list's matrices lie; y may be x; elements outside the matrices
  * are not touched).  mats, coeff: host, copied.  products: HS_FP32 for products as exact as in fp32, HS_BF16 for 16-bit products with 32-bit
- * sums (relative error about 1e-3 per matrix; both take any dtype).  The polynomials must keep the singular values below 3.9 and the
- * entries of b A + c A A below 60 in size.  A matrix with a value that is not finite becomes NaN as a whole; the others do not see it. */
+ * sums (relative error 0.5 to 2e-3 per matrix); both take any dtype.  The same call gives the same bits; how a matrix is rounded depends on the list
+ * it is in, whose sizes decide the kernels.  The polynomials must keep the singular values below 3.9 and the entries of b A + c A A below 60 in size.  A matrix with a value that is not finite becomes NaN as a whole; the others do not see it. */
 hs_status hs_op_orthogonalize(int32_t dtype, const void* x, void* y, size_t size, const hs_matrix* mats, int32_t n, int32_t products,
                               int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -195,10 +195,10 @@ __device__ __forceinline__ void mma_loop(int nk, unsigned char* lds_raw, f32x16 
 
 // For products of few tiles, where the chain of latencies through the contraction is what counts: every wave of the block forms the whole 32 x 32 tile over the
 // k-tiles w, w + NW, ..., from a ring of S stages of its own at `ring` and without a barrier; the tiles are added in wave order.  What comes back in acc is the sum,
-// in wave 0.  next(dst) requests the wave's next k-tile (or, once they are used up, something harmless); scales(t): the t-th one is about to be used (its scales in byte 0).
-template <class MMA, class TA, class TB, int NW, int S, class Next, class Scales>
-__device__ __forceinline__ void ks_loop(int nk, unsigned char* lds_raw, f32x16& acc, const int& sa, const int& sb, int lane, int wave, Next&& next,
-                                        Scales&& scales) {
+// in wave 0.  next(dst) requests the wave's next k-tile (or, once they are used up, something harmless).
+template <class MMA, class TA, class TB, int NW, int S, class Next>
+__device__ __forceinline__ void ks_loop(int nk, unsigned char* lds_raw, f32x16& acc, int lane, int wave, Next&& next) {
+  static_assert(!MMA::SCALED, "no scales");
   constexpr int KS = MMA::KS, STAGE = TA::BYTES + TB::BYTES, NL = TA::NI + TB::NI;
   unsigned char* const ring = lds_raw + wave * S * STAGE;
 #pragma unroll
@@ -212,14 +212,13 @@ __device__ __forceinline__ void ks_loop(int nk, unsigned char* lds_raw, f32x16& 
       wait_loads<(S - 2) * NL>();
       asm volatile("" ::: "memory");
       next(ring + ((u + S - 1) % S) * STAGE);      // its last reads are done: their results went into the last matrix instructions
-      scales(t);
       const bf16* sA = (const bf16*)(ring + u * STAGE);
       const bf16* sB = (const bf16*)(ring + u * STAGE + TA::BYTES);
       typename MMA::Frag fa[KS], fb[KS];
 #pragma unroll
       for (int k = 0; k < KS; ++k) { fa[k] = MMA::template frag<TA>(sA, 0, k, lane); fb[k] = MMA::template frag<TB>(sB, 0, k, lane); }
 #pragma unroll
-      for (int k = 0; k < KS; ++k) MMA::template mma<0>(MMA::template op<0>(fa[k], sa), MMA::template op<0>(fb[k], sb), acc, sa, sb);
+      for (int k = 0; k < KS; ++k) MMA::template mma<0>(fa[k], fb[k], acc, 0, 0);
     }
   }
   asm volatile("" ::: "memory");

@@ -53,7 +53,7 @@ struct NsDev {
   double* partial;         // [matrices][kParts]
   int from;                // which of the two X is read
 };
-static_assert(sizeof(NsDev) < 3072, "kernel arguments");
+static_assert(sizeof(NsDev) + 128 <= 4096, "kernel arguments");
 
 // parts of a matrix' workspace: two X of two numbers each, the square matrices (of two numbers each for 32-bit products), their diagonals
 __host__ __device__ inline size_t x_bytes(const NsGroup& g) { return (size_t)g.m * g.n * 4; }
@@ -87,7 +87,7 @@ __global__ void ns_table_kernel(TableArg t, NsPlace* __restrict__ table) {
 struct MuonIO {
   float *w, *m; const float* G; bf16* wl;
   float denom, mu, decay, lr, rms;      // denom 0: G as it is; decay = 1 - lr wd
-  int nesterov, scale;
+  int nesterov;
 };
 struct PlainIO { const void* x; void* y; int bf; };
 
@@ -272,7 +272,7 @@ __device__ __forceinline__ void to_f8(const f16x8& h, float (&x)[8]) {
 // GRAM: A = X X^T.  SYM: products of square matrices that commute (polynomials of A), whose diagonals are kept apart: with P = D + E and Q = D' + E' the
 // matrix instruction forms E E', and D E' + E D' + D D' are added on the way out.  Both are symmetric: tiles on and above the diagonal only, each
 // written in its place and mirrored.  APPLY: X <- (D + E) X, where X is read in 16 bits by the product with E and in full by D X.  LAST: the same on its way out.
-// bytes of LDS of a wave on the way out, and of a block
+// LDS in bytes: a wave's on the way out, and a block's.
 template <class C, int OP, bool SPLIT>
 constexpr int ns_wave_bytes() { return C::EPI_FLOATS * 4 + (OP == NS_GRAM || OP == NS_SYM ? (SPLIT ? 2 : 1) * 32 * (32 * C::TJ + 8) * 2 : 0); }
 template <class C, int OP, bool SPLIT>
@@ -445,7 +445,7 @@ void ns_product_kernel(NsDev d, IO io) {
 
   f32x16 acc[TI][TJ];
   clear_tiles(acc);
-  int sa[TI] = {}, sb[TJ] = {}, seg = 0;
+  int seg = 0;
   if constexpr (KSPLIT) {
     int kt = wave;
     auto next = [&](unsigned char* dst) __attribute__((always_inline)) {
@@ -456,7 +456,7 @@ void ns_product_kernel(NsDev d, IO io) {
       TB::issue(cb, dst + TA::BYTES, 0);
     };
     const int nk = nk1 * nseg;
-    ks_loop<MmaF16, TA, TB, C::KW, C::S>(nk > wave ? (nk - wave + C::KW - 1) / C::KW : 0, lds_raw, acc[0][0], sa[0], sb[0], lane, wave, next, [](int) {});
+    ks_loop<MmaF16, TA, TB, C::KW, C::S>(nk > wave ? (nk - wave + C::KW - 1) / C::KW : 0, lds_raw, acc[0][0], lane, wave, next);
     if (wave > 0) return;
   } else {
     int kt = 0;
@@ -466,6 +466,7 @@ void ns_product_kernel(NsDev d, IO io) {
       TA::issue(ca, dst, wave);
       TB::issue(cb, dst + TA::BYTES, wave);
     };
+    int sa[TI] = {}, sb[TJ] = {};      // no scales
     mma_loop<C, MmaF16, TA, TB>(nk1 * nseg, lds_raw, acc, sa, sb, wm, wn, lane, next, [](int) {});
   }
 
@@ -1037,7 +1038,7 @@ hipError_t ns_run(const std::vector<NsGroup>& groups, int kind, int split, char*
   };
   auto blocks_of = [&](auto per) {
     int64_t blocks = 0;
-      for (int i = 0; i < d.n; ++i) { d.first_block[i] = (int)blocks; blocks += (int64_t)d.job[i].g.count * per(d.job[i].g); }
+    for (int i = 0; i < d.n; ++i) { d.first_block[i] = (int)blocks; blocks += (int64_t)d.job[i].g.count * per(d.job[i].g); }
     d.first_block[d.n] = (int)blocks;
     return (unsigned)blocks;
   };
@@ -1105,7 +1106,7 @@ const double kDefaultCoeff[3] = {3.4445, -4.7750, 2.0315};
 
 template <class IO>
 hs_status orthogonalize_checked(const char* who, const IO& io, size_t size, const hs_matrix* mats, int32_t n, int32_t products, int32_t steps,
-                        const double* coeff, double eps, void* workspace, size_t workspace_bytes, hipStream_t s) {
+                                const double* coeff, double eps, void* workspace, size_t workspace_bytes, hipStream_t s) {
   const std::string name = std::string(who) + ": ";
   std::string why;
   if (products != HS_FP32 && products != HS_BF16) return hs_fail(nullptr, HS_ERR_INVALID_ARG, name + "products must be HS_FP32 or HS_BF16");
@@ -1200,7 +1201,7 @@ hs_status hs_muon_step(float* w, float* m, const float* G, void* w_lowp_out, siz
   if (!(momentum >= 0.0 && momentum < 1.0)) return hs_fail(nullptr, HS_ERR_INVALID_ARG, "hs_muon_step: momentum must be in [0, 1)");
   if (!std::isfinite(lr) || !std::isfinite(weight_decay) || !(rms >= 0.0) || std::isinf(rms))
     return hs_fail(nullptr, HS_ERR_INVALID_ARG, "hs_muon_step: lr and weight_decay must be finite, rms finite and >= 0");
-  const MuonIO io{w, m, G, (bf16*)w_lowp_out, (float)denom, (float)momentum, (float)(1.0 - lr * weight_decay), (float)lr, (float)rms, nesterov ? 1 : 0, 0};
+  const MuonIO io{w, m, G, (bf16*)w_lowp_out, (float)denom, (float)momentum, (float)(1.0 - lr * weight_decay), (float)lr, (float)rms, nesterov ? 1 : 0};
   return orthogonalize("hs_muon_step", io, size, mats, n, products, steps, coeff, eps, workspace, workspace_bytes, (hipStream_t)stream);
 }
 

@@ -27,9 +27,21 @@ def tolerance(x, products, runs=None, **kw):
     sums.  (The sums have to be in it: 513 in 32-bit products are 97 additions of up to 2^-24 of the running sum each, which together are more than the
     2^-23 of a number kept in 22 bits.)  Twice that, for sums in another order; at least 8 of 22 bits.  Roundings that fall otherwise: the
     error is that of k = min(rows, cols) directions, each of which its own amplification makes a sum of few, so both norms are samples of a
-    distribution with k degrees of freedom, three of whose standard deviations are 3 / sqrt(2 k) of it; 3 / sqrt(k) for the two."""
+    distribution with k degrees of freedom, three of whose standard deviations are 3 / sqrt(2 k) of it; 3 / sqrt(k) for the two.
+    With few directions one sample says nothing about that: for k = 2 the ratio of two squared norms exceeds f with probability 1 / (1 + f), that is 2.5 % for
+    the factor 2 (1 + 3 / sqrt(2)) = 6.2 on the norms, in every one of hundreds of matrices.  Up to 16 directions the oracle's norm is therefore the root mean
+    square over 16 reflections of the matrix, which have its singular values and roundings of their own: 1 / (1 + f / 16)^16 = 3e-9."""
     e = M.orthogonalize(x, **kw)
-    return max(2.0 * (1.0 + 3.0 / np.sqrt(min(x.shape))) * rel(M.orthogonalize(x, numbers=1 if products == 1 else 2, runs=runs, **kw), e), 8 * 2.0 ** -22), e
+    numbers, k = 1 if products == 1 else 2, min(x.shape)
+    emulated = rel(M.orthogonalize(x, numbers=numbers, runs=runs, **kw), e)
+    if k <= 16:
+        rng, squares = np.random.default_rng(x.shape[0] * 10007 + x.shape[1]), 0.0
+        for _ in range(16):
+            v = rng.standard_normal(max(x.shape))      # of the longer side
+            other = (x - np.outer(x @ v, v) * (2.0 / (v @ v))) if x.shape[1] == v.size else x - np.outer(v, v @ x) * (2.0 / (v @ v))
+            squares += rel(M.orthogonalize(other, numbers=numbers, runs=runs, **kw), M.orthogonalize(other, **kw)) ** 2 / 16
+        emulated = max(emulated, np.sqrt(squares))
+    return max(2.0 * (1.0 + 3.0 / np.sqrt(k)) * emulated, 8 * 2.0 ** -22), e
 
 
 def layout(shapes, gap=0, ld=0):
