@@ -333,7 +333,8 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
  * dtype: element type of x and y (flat buffers of `size` elements, in which the list's matrices lie; y may be x; elements outside the matrices
  * are not touched).  mats, coeff: host, copied.  products: HS_FP32 for products as exact as in fp32, HS_BF16 for 16-bit products with 32-bit
  * sums (relative error 0.5 to 2e-3 per matrix); both take any dtype.  The same call gives the same bits; how a matrix is rounded depends on the list
- * it is in, whose sizes decide the kernels.  The polynomials must keep the singular values below 3.9 and the entries of b A + c A A below 60 in size.  A matrix with a value that is not finite becomes NaN as a whole; the others do not see it. */
+ * it is in, whose sizes decide the kernels.  The polynomials must keep the singular values below 3.9 and the entries of b A + c A A below 60 in size.
+ * A matrix with a value that is not finite becomes NaN as a whole; the others do not see it. */
 hs_status hs_op_orthogonalize(int32_t dtype, const void* x, void* y, size_t size, const hs_matrix* mats, int32_t n, int32_t products,
                               int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);
 
@@ -479,7 +480,9 @@ hs_status hs_op_quantize_fp8(int32_t dtype, const void* x, int64_t ldx, int32_t 
                              uint8_t* qs, int64_t ldqs, void* qt, int64_t ldqt, uint8_t* qts, int64_t ldqts, void* stream);
 /* C[M,N] = sum_k A(m,k) B(n,k) of such operands, with 32-bit sums; C is float (c_f32 != 0; C = beta C + sum, beta == 0 does not read C) or
  * bfloat16; bias [N] bfloat16 or NULL.  Row strides of codes multiples of 128 and at most 4 MiB, of scales multiples of 4.  scratch (dev, may
- * be NULL) as in hs_op_gemm: with it, contractions of products with few tiles are split and the partial sums added in a fixed order. */
+ * be NULL) as in hs_op_gemm: with it, contractions of products with few tiles are split and the partial sums added in a fixed order.
+ * For float results every code times its scale is held as a bfloat16: exact for scale bytes 3 .. 246, while 0 .. 2 round to its multiples of 2^-133 and
+ * 247 on (values from 448 2^119 on) may become infinite; bfloat16 results take every scale byte. */
 hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, const uint8_t* as, int64_t ldas, const void* B,
                          int64_t ldb, const uint8_t* bs, int64_t ldbs, void* C, int64_t ldc, int32_t c_f32, float beta,
                          const void* bias, void* scratch, size_t scratch_bytes, void* stream);

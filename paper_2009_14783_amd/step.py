@@ -39,10 +39,18 @@ class MatrixUpdate:
         self.bytes = hs.hs_orthogonalize_workspace_bytes(self.mats, self.products)
         self.ws = torch.empty(self.bytes, dtype=torch.uint8, device=device)
 
+    @classmethod
+    def options(cls, muon: dict, adam: dict) -> dict:
+        o = dict(cls.DEFAULTS, lr=adam["lr"])
+        unknown = set(muon) - set(o)
+        if unknown:
+            raise TypeError(f"muon: unknown arguments {sorted(unknown)}")
+        return dict(o, **muon)
+
     def apply(self, worker, denom: float, adam: dict, muon: dict, t: int):
         """Update number t of all parameters with the gradient sums in worker.G.  Adam's share of G is divided by denom in place; the matrices' share stays."""
-        o = dict(self.DEFAULTS, **muon)
-        hs.hs_muon_step(worker.w, worker.m, worker.G, worker.w_lowp, worker.P, self.mats, self.products, denom, o.get("lr", adam["lr"]), o["momentum"],
+        o = self.options(muon, adam)
+        hs.hs_muon_step(worker.w, worker.m, worker.G, worker.w_lowp, worker.P, self.mats, self.products, denom, o["lr"], o["momentum"],
                         1 if o["nesterov"] else 0, o["weight_decay"], o["rms"], o["steps"], o["coeff"], o["eps"], self.ws, self.bytes)
         for off, n in self.ranges:
             w, m, v, G = (t[off:off + n] for t in (worker.w, worker.m, worker.v, worker.G))
@@ -200,6 +208,7 @@ class Worker:
         muon: weight matrices are updated by their orthogonalised momentum behind the backward pass (hs_muon_step), the other
         parameters by Adam; a dict of the arguments of MatrixUpdate.DEFAULTS that are to differ, and "lr" (adam's if absent)."""
         if muon is not None:
+            MatrixUpdate.options(muon, adam)      # refused before anything is done
             n_total = self.accumulate_micro_batches(batches, fused)
             D = n_total if denom is None else denom
             self.matrices.apply(self, float(D), adam, muon, self.t + 1)
@@ -379,6 +388,8 @@ class PairWorker:
         the pass (ms per step of the base model: 320 rows per side 2.15 -> 1.96, 4096 4.18 -> 4.08, 8064 6.71 -> 6.65).  muon: as in Worker.train_step; the update
         is then behind the pass."""
         assert len(batches) <= 64
+        if muon is not None:
+            MatrixUpdate.options(muon, adam)      # refused before anything is done
         hs.hs_fill_zero(self.loss_buf, 4 * self.loss_buf.numel())
         real = [i for i, d in enumerate(batches) if d is not None]
         D = float(denom if denom is not None else max(sum(batches[i]["n_tok"] for i in real), 1))

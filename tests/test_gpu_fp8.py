@@ -206,6 +206,32 @@ def test_scales_far_from_one(hs, e):
     assert np.all(np.abs(c.cpu().double().numpy() - want) <= 258 * 2.0 ** -24 * size)
 
 
+@pytest.mark.parametrize("ea,eb", [(3, 220), (220, 3), (246, 4), (4, 246), (20, 100)])
+def test_smallest_and_largest_scales_of_float_results(hs, ea, eb):
+    """Code times scale is a multiple of 2^(e - 136), which a bfloat16 holds from 2^-133 on, and at most 448 2^(e - 127), below 2^128 up to e = 246."""
+    rng = np.random.default_rng(13)
+    a, sa = operand(rng, 40, 256, 1)
+    b, sb = operand(rng, 50, 256, 1)
+    sa[:, :2], sb[:, :2] = ea, eb
+    c = torch.empty(40, 50, device="cuda")
+    product(hs, 40, 50, 256, *dev(a, sa, b, sb), c, 50, c_f32=1)
+    want, size = M.gemm_fp8(a, sa, b, sb, 256)
+    assert np.all(np.abs(c.cpu().double().numpy() - want) <= 258 * 2.0 ** -24 * size)
+
+
+@pytest.mark.parametrize("ea,eb", [(0, 220), (220, 0), (10, 240), (254, 0), (0, 254)])
+def test_smallest_and_largest_scales_of_bfloat16_results(hs, ea, eb):
+    """Bounds as in test_product_against_the_oracle."""
+    rng = np.random.default_rng(14)
+    a, sa = operand(rng, 40, 256, 1)
+    b, sb = operand(rng, 50, 256, 1)
+    sa[:, :2], sb[:, :2] = ea, eb
+    o = torch.empty(40, 50, dtype=torch.bfloat16, device="cuda")
+    product(hs, 40, 50, 256, *dev(a, sa, b, sb), o, 50)
+    want, size = M.gemm_fp8(a, sa, b, sb, 256)
+    assert np.all(np.abs(o.cpu().double().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 1.01 * (2.0 ** -9 + 258 * 2.0 ** -24) * size)
+
+
 def test_rows_with_room_between_them(hs):
     rng = np.random.default_rng(2)
     m, n, k = 100, 140, 300

@@ -109,3 +109,12 @@ def test_columns_of_one_wider_matrix_are_a_fine_list():
     """What is refused for sharing elements is told apart from neighbours: the call gets as far as its workspace."""
     mats = [(0, 12, 4, 5), (5, 12, 4, 7), (48, 12, 2, 12)]
     refused(WORKSPACE, hs.hs_op_orthogonalize, *ortho(mats=mats, size=72, nbytes=100))
+
+
+def test_options_of_the_workers():
+    from paper_2009_14783_amd.step import MatrixUpdate
+    o = MatrixUpdate.options(dict(momentum=0.9), dict(lr=1e-4))
+    assert o == dict(MatrixUpdate.DEFAULTS, momentum=0.9, lr=1e-4)
+    assert MatrixUpdate.options(dict(lr=1e-3), dict(lr=1e-4))["lr"] == 1e-3
+    with pytest.raises(TypeError, match="momentun"):
+        MatrixUpdate.options(dict(momentun=0.9), dict(lr=1e-4))
