@@ -49,11 +49,10 @@ struct NsDev {
   int first_block[kJobs + 1];
   NsJob job[kJobs];
   char* ws;
-  const NsPlace* table;
+  NsPlace* table;
   double* partial;         // [matrices][kParts]
   int from;                // which of the two X is read
 };
-static_assert(sizeof(NsDev) + 128 <= 4096, "kernel arguments");
 
 // parts of a matrix' workspace: two X of two numbers each, the square matrices (of two numbers each for 32-bit products), their diagonals
 __host__ __device__ inline size_t x_bytes(const NsGroup& g) { return (size_t)g.m * g.n * 4; }
@@ -76,7 +75,12 @@ __device__ __forceinline__ int ns_job(const NsDev& d, int v) {
   return i;
 }
 
-struct TableArg { NsPlace place[200]; int first, n; };
+// The places travel as kernel arguments: those of short lists with the first pass, which writes them into the table for the launches behind it (a launch less: one
+// matrix 130 x 67 71.1 -> 69.6 us, toy model 114.5 -> 113.1); those of longer ones with launches of their own.
+template <int N>
+struct Places { NsPlace place[N]; int first, n; };
+typedef Places<200> TableArg;
+typedef Places<100> ShortTable;
 __global__ void ns_table_kernel(TableArg t, NsPlace* __restrict__ table) {
   const int i = threadIdx.x;
   if (i < t.n) table[t.first + i] = t.place[i];
@@ -158,11 +162,12 @@ __device__ __forceinline__ void emit4(const PlainIO& io, int64_t i, int have, bo
 // First pass: the momentum is updated, and the sum of squares of what is going to be orthogonalised is formed in 64 bits (gradients of 1e-25 have squares
 // that 32 bits do not hold), a part of a matrix per block, added in a fixed order.  Memory bound: 12 bytes per element.
 template <class IO>
-__global__ __launch_bounds__(256) void ns_norm_kernel(NsDev d, IO io) {
+__global__ __launch_bounds__(256) void ns_norm_kernel(NsDev d, IO io, ShortTable t) {
   const int ji = ns_job(d, blockIdx.x);
   const NsGroup& g = d.job[ji].g;
   const int local = blockIdx.x - d.first_block[ji], mat = local / g.parts, part = local % g.parts;
-  const NsPlace at = d.table[g.first + mat];
+  const NsPlace at = t.n > 0 ? t.place[g.first + mat] : d.table[g.first + mat];
+  if (t.n > 0 && part == 0 && threadIdx.x == 0) d.table[g.first + mat] = at;
   // a matrix without gaps is one long row
   const bool flat = at.ld == g.cols;
   const int cols = flat ? g.rows * g.cols : g.cols, per_row = (cols + 3) / 4, total = (flat ? 1 : g.rows) * per_row;
@@ -915,7 +920,7 @@ hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
 constexpr double kGramAlone = 1.5e10, kGramBeside = 8e10;
 
 // Whether a list goes through the panel kernel: up to 128 rows in every matrix, blocks for about one round of the chip, and not too much to read of each other's
-// parts of A (a matrix of P panels: P P m m floats in a step).  Whole list in us, with and without: 130 x 67 in 32 bits 72, 107; 64 x 64 42, 94; 16 of
+// parts of A (a matrix of P panels: P P m m floats in a step).  Whole list in us, with and without: 130 x 67 in 32 bits 70, 107; 64 x 64 42, 94; 16 of
 // 64 x 1024 (64 MB) 77, 106, 64 of them 223, 142; 24 layers of hidden 64 (288 blocks) 89, 107, 48 of them 132, 122; of 128 rows, whose steps are longer: toy model
 // 113, 121 (9 MB); 16 of 128 x 256 (17 MB) 94, 99; 16 of 128 x 512 (67 MB) 127, 103.
 bool ns_small(const std::vector<NsGroup>& groups) {
@@ -1029,8 +1034,9 @@ hipError_t launch_panel(const NsDev& d, const IO& io, double eps, unsigned block
 
 // The whole of it for groups that go the same way.
 template <class IO>
-hipError_t ns_run(const std::vector<NsGroup>& groups, int kind, int split, char* ws, const NsPlace* table, double* partial, const IO& io, int steps,
-                  const double* c, double eps, hipStream_t s) {
+hipError_t ns_run(const std::vector<NsGroup>& groups, int kind, int split, char* ws, NsPlace* table, const ShortTable& places, double* partial, const IO& io,
+                  int steps, const double* c, double eps, hipStream_t s) {
+  static_assert(sizeof(NsDev) + sizeof(ShortTable) + sizeof(IO) + 64 <= 4096, "kernel arguments");
   NsDev d{};
   d.split = split; d.ws = ws; d.table = table; d.partial = partial;
   auto add = [&](int p, int q, int out, double ident, double alpha, double beta) {
@@ -1044,7 +1050,7 @@ hipError_t ns_run(const std::vector<NsGroup>& groups, int kind, int split, char*
   };
   add(0, 0, 0, 0.0, 0.0, 0.0);
   unsigned blocks = blocks_of([](const NsGroup& g) { return g.parts; });
-  hipLaunchKernelGGL(ns_norm_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io);
+  hipLaunchKernelGGL(ns_norm_kernel<IO>, dim3(blocks), dim3(256), 0, s, d, io, places);
   if (kind == NS_BY_PANEL) {
     blocks = blocks_of([](const NsGroup& g) { return g.n / kPanel; });
     hipError_t e = split ? launch_panel<true, PANEL_FIRST>(d, io, eps, blocks, s) : launch_panel<false, PANEL_FIRST>(d, io, eps, blocks, s);
@@ -1128,11 +1134,15 @@ hs_status orthogonalize_checked(const char* who, const IO& io, size_t size, cons
   if ((uintptr_t)workspace % 256) return hs_fail(nullptr, HS_ERR_INVALID_ARG, name + "workspace must be 256-byte aligned");
   char* const ws = (char*)workspace;
   NsPlace* const table = (NsPlace*)(ws + plan.table);
+  auto place = [&](int i) { return NsPlace{mats[plan.order[i]].offset, mats[plan.order[i]].ld}; };
   hipError_t e = hipSuccess;
-  for (int done = 0; done < n && e == hipSuccess; done += 200) {
+  ShortTable places{};
+  places.first = 0; places.n = n <= 100 ? n : 0;
+  for (int i = 0; i < places.n; ++i) places.place[i] = place(i);
+  for (int done = 0; places.n == 0 && done < n && e == hipSuccess; done += 200) {
     TableArg t;
     t.first = done; t.n = std::min(200, n - done);
-    for (int i = 0; i < t.n; ++i) t.place[i] = NsPlace{mats[plan.order[done + i]].offset, mats[plan.order[done + i]].ld};
+    for (int i = 0; i < t.n; ++i) t.place[i] = place(done + i);
     hipLaunchKernelGGL(ns_table_kernel, dim3(1), dim3(256), 0, s, t, table);
     e = hipGetLastError();
   }
@@ -1144,7 +1154,7 @@ hs_status orthogonalize_checked(const char* who, const IO& io, size_t size, cons
     const size_t most = kind == NS_BY_GRAM ? kJobs / 2 : kJobs;      // two products of a group in one launch
     for (size_t i = 0; i <= plan.groups.size() && e == hipSuccess; ++i) {
       if (!now.empty() && (i == plan.groups.size() || now.size() == most)) {
-        e = ns_run(now, kind, split, ws, table, (double*)(ws + plan.partial), io, steps, c.data(), eps, s);
+        e = ns_run(now, kind, split, ws, table, places, (double*)(ws + plan.partial), io, steps, c.data(), eps, s);
         now.clear();
       }
       if (i < plan.groups.size() && plan.groups[i].kind == kind) now.push_back(plan.groups[i]);
