@@ -320,3 +320,32 @@ def test_refusals_leave_the_output_alone(hs):
         hs.hs_op_quantize_fp8(0, c, 4, 4, 4, 0, q, 100, s, 4)
     torch.cuda.synchronize()
     assert torch.all(c == 3.0) and torch.all(q == 0)
+
+
+def test_places_beyond_32_bits(hs):
+    """A result of more than 2^32 elements, and rows of the quantiser's input that lie up to 2^32 elements apart."""
+    rng = np.random.default_rng(15)
+    m, n, k = 66000, 66000, 128
+    a, sa = operand(rng, 128, k, 1)
+    b, sb = operand(rng, 96, k, 1)
+    rows, cols = np.arange(m) % 128, np.arange(n) % 96
+    da, dsa, db, dsb = dev(a[rows], sa[rows], b[cols], sb[cols])
+    c = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    product(hs, m, n, k, da, dsa, db, dsb, c, n)
+    want, size = M.gemm_fp8(a, sa, b, sb, k)
+    for i, j in ((0, 0), (m - 256, 0), (0, n - 192), (m - 256, n - 192), (m // 2, n // 2)):
+        got = c[i:i + 256, j:j + 192].cpu().double().numpy()
+        w, z = want[np.ix_(rows[i:i + 256], cols[j:j + 192])], size[np.ix_(rows[i:i + 256], cols[j:j + 192])]
+        assert np.all(np.abs(got - w) <= 2.0 ** -8 * np.abs(w) + 1.01 * (2.0 ** -9 + 130 * 2.0 ** -24) * z)
+    ld, R, C = 1 << 27, 40, 200
+    del c
+    x = torch.empty((R - 1) * ld + C, dtype=torch.bfloat16, device="cuda")
+    h = rng.standard_normal((R, C)).astype(np.float32)
+    view = x.as_strided((R, C), (ld, 1))
+    view.copy_(torch.from_numpy(h))
+    q = torch.zeros(R, 256, dtype=torch.uint8, device="cuda")
+    s = torch.zeros(R, 2, dtype=torch.uint8, device="cuda")
+    hs.hs_op_quantize_fp8(1, x, ld, R, C, 0, q, 256, s, 2, None, 128, None, 1)
+    torch.cuda.synchronize()
+    wq, ws = M.quantize(view.cpu().double().numpy())
+    assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws)

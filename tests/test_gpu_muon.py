@@ -429,3 +429,25 @@ def test_step_without_data_and_loop(hs):
     off, r, c = next((o, r, c) for name, o, r, c in lay if name == "l0.o.w")
     assert torch.allclose(worker.m[off:off + r * c], 0.9 * m[off:off + r * c], rtol=2.0 ** -23, atol=0)
     worker.close()
+
+
+@pytest.mark.parametrize("shape", [(60, 90), (300, 200)])
+def test_places_beyond_32_bits(hs, shape):
+    """Matrices that start behind 2^32 elements, and whose rows are 2^25 elements apart."""
+    rng = np.random.default_rng(16)
+    r, c = shape
+    ld = 1 << 25
+    mats = [((1 << 32) + 4, c, r, c), ((1 << 32) + (1 << 20), ld, r, c)]
+    size = mats[1][0] + (r - 1) * ld + c
+    x = torch.empty(size, dtype=torch.bfloat16, device="cuda")
+    views = [x.as_strided((r, c), (m[1], 1), m[0]) for m in mats]
+    host = []
+    for v in views:
+        v.copy_(torch.from_numpy(rng.standard_normal(shape).astype(np.float32)))
+        host.append(v.cpu().double().numpy())
+    lst = hs.make_matrices(mats)
+    ws, n = workspace(hs, lst, 0)
+    hs.hs_op_orthogonalize(1, x, x, size, lst, 0, 5, None, 1e-7, ws, n)
+    for v, h in zip(views, host):
+        tol, e = tolerance(h, 0)
+        assert rel(v.cpu().double().numpy(), e) <= tol + 2.0 ** -8, shape      # bf16 results
