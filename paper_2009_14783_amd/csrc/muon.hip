@@ -996,8 +996,27 @@ bool ns_list_ok(const hs_matrix* mats, int32_t n, std::string* why) {
   return true;
 }
 
-// Whether two matrices of the list share an element: neighbours in the order of their offsets whose ranges meet may only be columns of one wider
-// matrix (the same row stride, other columns).
+// Whether two matrices share an element, a starting where b does or before and reaching beyond b's first.  With one row stride all rows of b lie alike
+// between those of a; otherwise every row of the one with fewer rows is looked up among the other's.
+bool ns_share(const hs_matrix& a, const hs_matrix& b) {
+  if (a.ld == b.ld) {
+    const int64_t shift = (b.offset - a.offset) % a.ld;      // b's first column, counted from a's
+    return shift < a.cols || shift + b.cols > a.ld;
+  }
+  const hs_matrix& few = a.rows < b.rows ? a : b;
+  const hs_matrix& many = a.rows < b.rows ? b : a;
+  for (int64_t i = 0; i < few.rows; ++i) {
+    const int64_t first = few.offset + i * few.ld - many.offset, last = first + few.cols;      // of this row, counted from the other matrix
+    if (last <= 0) continue;
+    if (first < 0) return true;
+    const int64_t k = first / many.ld;                       // the other's row that starts here or before
+    if (k >= many.rows) break;
+    if (first - k * many.ld < many.cols || (k + 1 < many.rows && (k + 1) * many.ld < last)) return true;
+  }
+  return false;
+}
+
+// Whether no two matrices of the list share an element.
 bool ns_disjoint(const hs_matrix* mats, int n) {
   std::vector<int> order(n);
   std::iota(order.begin(), order.end(), 0);
@@ -1005,14 +1024,8 @@ bool ns_disjoint(const hs_matrix* mats, int n) {
   auto end = [&](const hs_matrix& a) { return a.offset + (a.rows - 1) * a.ld + a.cols; };
   std::vector<int> open;      // matrices that reach beyond the present offset
   for (int i : order) {
-    const hs_matrix& b = mats[i];
-    open.erase(std::remove_if(open.begin(), open.end(), [&](int k) { return end(mats[k]) <= b.offset; }), open.end());
-    for (int k : open) {
-      const hs_matrix& a = mats[k];
-      if (a.ld != b.ld) return false;
-      const int64_t shift = (b.offset - a.offset) % a.ld;      // b's first column, counted from a's
-      if (shift < a.cols || shift + b.cols > a.ld) return false;
-    }
+    open.erase(std::remove_if(open.begin(), open.end(), [&](int k) { return end(mats[k]) <= mats[i].offset; }), open.end());
+    for (int k : open) if (ns_share(mats[k], mats[i])) return false;
     open.push_back(i);
   }
   return true;

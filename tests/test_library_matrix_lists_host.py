@@ -1,0 +1,59 @@
+"""Lists of matrices that the matrix update takes or refuses, on the host: a list is taken if no element is in it twice, wherever its matrices lie.
+A list that is taken gets as far as its workspace, which is too small here."""
+import numpy as np
+import pytest
+
+from paper_2009_14783_amd import binding as hs
+
+P = 1 << 20          # a stand-in for an aligned device address; no call here gets as far as using one
+INVALID, WORKSPACE = 1, 3
+
+
+def status_of(mats, size=1 << 40):
+    with pytest.raises(hs.HsError) as e:
+        hs.hs_op_orthogonalize(0, P, P, size, hs.make_matrices(mats), 0, 5, None, 1e-7, P, 100, stream=0)
+    return e.value.status
+
+
+@pytest.mark.parametrize("mats", [
+    [(0, 100, 2, 10), (20, 10, 2, 10)],                        # whole in the gap of the other
+    [(20, 10, 2, 10), (0, 100, 2, 10)],
+    [(0, 100, 2, 50), (50, 50, 1, 50)],                        # one row in a gap: its own stride means nothing
+    [(0, 100, 3, 10), (150, 7, 6, 7), (10, 90, 1, 90)],
+    [(0, 10, 4, 3), (3, 20, 2, 7), (13, 20, 2, 7)],            # every second gap
+    [(0, 7, 9, 2), (2, 21, 3, 5)],
+    [(0, 100, 2, 10), (20, 45, 3, 10)],                        # the third row starts right behind the other's second
+    [(5, 11, 3, 4), (0, 40, 2, 5)]])                           # the longer stride starts first and ends last
+def test_neighbours_of_other_strides_are_taken(mats):
+    assert status_of(mats) == WORKSPACE
+
+
+@pytest.mark.parametrize("mats", [
+    [(0, 100, 2, 10), (20, 90, 2, 10), (105, 100, 1, 1)],
+    [(0, 100, 2, 50), (50, 51, 1, 51)],                        # the row reaches one element into the next
+    [(0, 10, 4, 3), (3, 19, 3, 7)],                            # the second row starts at 22, on the other's third
+    [(0, 7, 9, 2), (2, 22, 3, 5)],
+    [(0, 100, 2, 10), (95, 6, 1, 6)],
+    [(0, 100, 2, 10), (20, 44, 3, 10)]])                       # the third row, 108 .. 117, on the other's 100 .. 109
+def test_neighbours_of_other_strides_that_share_an_element_are_refused(mats):
+    assert status_of(mats) == INVALID
+
+
+def test_random_lists_against_their_elements():
+    rng = np.random.default_rng(3)
+    seen = set()
+    for _ in range(3000):
+        mats, used, twice = [], set(), False
+        for _ in range(int(rng.integers(2, 4))):
+            r, c = int(rng.integers(1, 6)), int(rng.integers(1, 8))
+            ld = int(rng.choice([c, c + int(rng.integers(0, 30)), 24]))
+            if ld < c:
+                ld = c
+            off = int(rng.integers(0, 40))
+            mats.append((off, ld, r, c))
+            mine = {off + i * ld + j for i in range(r) for j in range(c)}
+            twice = twice or bool(mine & used)
+            used |= mine
+        assert status_of(mats) == (INVALID if twice else WORKSPACE), mats
+        seen.add(twice)
+    assert seen == {False, True}
