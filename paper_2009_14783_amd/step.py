@@ -47,9 +47,22 @@ class MatrixUpdate:
             raise TypeError(f"muon: unknown arguments {sorted(unknown)}")
         return dict(o, **muon)
 
+    @classmethod
+    def check(cls, muon: dict, adam: dict, denom: float, compute: int) -> dict:
+        """options(), once everything that one of an update's calls would refuse has been looked at: they come one after the other, and what the
+        second refuses must not leave the first one's parameters updated.  Launches nothing."""
+        o = cls.options(muon, adam)
+        hs.hs_muon_step(None, None, None, None, 0, hs.make_matrices([]), compute, float(denom), o["lr"], o["momentum"], 1 if o["nesterov"] else 0,
+                        o["weight_decay"], o["rms"], o["steps"], o["coeff"], o["eps"], None, 0, stream=0)      # an empty list: checks only
+        beta1, beta2, eps = (float(adam[k]) for k in ("beta1", "beta2", "eps"))
+        float(adam["lr"]), float(adam.get("weight_decay", 0.0))
+        if not (0.0 <= beta1 < 1.0 and 0.0 <= beta2 < 1.0 and eps >= 0.0):
+            raise hs.HsError(1, "adam: betas must be in [0,1), eps >= 0")
+        return o
+
     def apply(self, worker, denom: float, adam: dict, muon: dict, t: int):
         """Update number t of all parameters with the gradient sums in worker.G.  Adam's share of G is divided by denom in place; the matrices' share stays."""
-        o = self.options(muon, adam)
+        o = self.check(muon, adam, denom, self.products)
         hs.hs_muon_step(worker.w, worker.m, worker.G, worker.w_lowp, worker.P, self.mats, self.products, denom, o["lr"], o["momentum"],
                         1 if o["nesterov"] else 0, o["weight_decay"], o["rms"], o["steps"], o["coeff"], o["eps"], self.ws, self.bytes)
         for off, n in self.ranges:
@@ -208,9 +221,9 @@ class Worker:
         muon: weight matrices are updated by their orthogonalised momentum behind the backward pass (hs_muon_step), the other
         parameters by Adam; a dict of the arguments of MatrixUpdate.DEFAULTS that are to differ, and "lr" (adam's if absent)."""
         if muon is not None:
-            MatrixUpdate.options(muon, adam)      # refused before anything is done
-            n_total = self.accumulate_micro_batches(batches, fused)
-            D = n_total if denom is None else denom
+            D = sum(d["n_seq"] for d in batches if d is not None and not d.get("dummy", False)) if denom is None else denom
+            MatrixUpdate.check(muon, adam, D, self.compute)      # refused before anything is done
+            self.accumulate_micro_batches(batches, fused)
             self.matrices.apply(self, float(D), adam, muon, self.t + 1)
             self.t += 1
             return D
@@ -388,11 +401,11 @@ class PairWorker:
         the pass (ms per step of the base model: 320 rows per side 2.15 -> 1.96, 4096 4.18 -> 4.08, 8064 6.71 -> 6.65).  muon: as in Worker.train_step; the update
         is then behind the pass."""
         assert len(batches) <= 64
-        if muon is not None:
-            MatrixUpdate.options(muon, adam)      # refused before anything is done
-        hs.hs_fill_zero(self.loss_buf, 4 * self.loss_buf.numel())
         real = [i for i, d in enumerate(batches) if d is not None]
         D = float(denom if denom is not None else max(sum(batches[i]["n_tok"] for i in real), 1))
+        if muon is not None:
+            MatrixUpdate.check(muon, adam, D, self.compute)      # refused before anything is done
+        hs.hs_fill_zero(self.loss_buf, 4 * self.loss_buf.numel())
         self.t += 1
         first, in_backward = True, self.P >= 4 << 20 if update_in_backward is None else update_in_backward
         in_backward = in_backward and muon is None
