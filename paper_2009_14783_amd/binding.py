@@ -150,7 +150,11 @@ def _ptr(t):
     try:
         return t.data_ptr()      # tensors first: a call passes up to nine of them
     except AttributeError:
-        return t.ctypes.data if isinstance(t, np.ndarray) else t
+        if isinstance(t, np.ndarray):
+            return t.ctypes.data
+        if isinstance(t, int):
+            return t
+        raise                    # ctypes would take the address of a string
 
 
 def _stream(stream):
