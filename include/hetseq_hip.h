@@ -322,7 +322,7 @@ typedef struct {
   int32_t rows, cols;
 } hs_matrix;
 
-/* Bytes of scratch that hs_op_orthogonalize / hs_muon_step need for a list (0 for an invalid one).  Calls that overlap in time, and
+/* Bytes of scratch that hs_op_orthogonalize / hs_muon_step need for a list (0 for an invalid one, never for an empty one).  Calls that overlap in time, and
  * captured graphs that may, need a workspace each; nothing in it has to start at zero and nothing of it is kept for the next call. */
 size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_t products);
 

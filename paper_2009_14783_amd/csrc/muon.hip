@@ -1198,7 +1198,7 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
     return 0;
   }
   try {
-    return ns_plan(mats, n, products == HS_FP32).total;
+    return std::max<size_t>(ns_plan(mats, n, products == HS_FP32).total, 256);      // an empty list is no invalid one
   } catch (const std::bad_alloc&) {
     hs_fail(nullptr, HS_ERR_STATE, "hs_orthogonalize_workspace_bytes: out of host memory");
     return 0;

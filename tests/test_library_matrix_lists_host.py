@@ -57,3 +57,12 @@ def test_random_lists_against_their_elements():
         assert status_of(mats) == (INVALID if twice else WORKSPACE), mats
         seen.add(twice)
     assert seen == {False, True}
+
+
+def test_an_empty_list_is_no_error():
+    for products in (0, 1):
+        n = hs.hs_orthogonalize_workspace_bytes(hs.make_matrices([]), products)
+        assert n > 0
+        hs.hs_op_orthogonalize(0, None, None, 0, hs.make_matrices([]), products, 5, None, 1e-7, None, n, stream=0)
+    with pytest.raises(hs.HsError):
+        hs.hs_orthogonalize_workspace_bytes(hs.make_matrices([]), 7)
