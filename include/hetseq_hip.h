@@ -338,6 +338,10 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
 hs_status hs_op_orthogonalize(int32_t dtype, const void* x, void* y, size_t size, const hs_matrix* mats, int32_t n, int32_t products,
                               int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);
 
+/* How matrix number `matrix` of a list is gone about: *way 0 products with X in every step, 1 polynomials of A with X in every third, 2 a launch
+ * per step (small matrices); tiles [3]: the side of the tiles (32 .. 256; 0 for way 2) of X X^T, of one product of symmetric matrices, and of S X.  Host only, no GPU needed. */
+hs_status hs_orthogonalize_choice(const hs_matrix* mats, int32_t n, int32_t products, int32_t matrix, int32_t* way, int32_t* tiles);
+
 /* One update of the list's matrices.  g = G / denom (denom == 0: G), m = momentum m + g, u = g + momentum m (nesterov != 0) or m,
  * w = (1 - lr weight_decay) w - lr s O(u) with O as in hs_op_orthogonalize and s = rms sqrt(max(rows, cols)), which makes the root
  * mean square of the update rms times lr whatever the shape (rms > 0; 0.2 goes with learning rates made for Adam), or
@@ -486,6 +490,10 @@ hs_status hs_op_quantize_fp8(int32_t dtype, const void* x, int64_t ldx, int32_t 
 hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, const uint8_t* as, int64_t ldas, const void* B,
                          int64_t ldb, const uint8_t* bs, int64_t ldbs, void* C, int64_t ldc, int32_t c_f32, float beta,
                          const void* bias, void* scratch, size_t scratch_bytes, void* stream);
+
+/* How hs_op_gemm_fp8 goes about a product with so many bytes of scratch: the side of its block tiles (64, 128, 256) and into how many parts it splits the
+ * contraction.  Host only, no GPU needed. */
+hs_status hs_gemm_fp8_choice(int32_t M, int32_t N, int32_t K, int32_t c_f32, size_t scratch_bytes, int32_t* tile, int32_t* splits);
 
 /* Timing aid, not part of the method: the library holds several tilings of its bf16 GEMM kernel (numbered 0 .. 11: block
  * tile, k-tile depth, blocks per CU, operands staged through registers or loaded into LDS directly, contraction split

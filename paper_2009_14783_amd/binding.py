@@ -71,6 +71,7 @@ _SIGNATURES = {
     "hs_adam_step": (_I32, [_P, _P, _P, _P, _P, _SZ, _D, _D, _D, _D, _D, _I64, _P]),
     "hs_normalize_adam_step": (_I32, [_P, _P, _P, _P, _P, _SZ, _D, _D, _D, _D, _D, _D, _I64, _P]),
     "hs_orthogonalize_workspace_bytes": (_SZ, [_P, _I32, _I32]),
+    "hs_orthogonalize_choice": (_I32, [_P, _I32, _I32, _I32, C.POINTER(_I32), C.POINTER(_I32)]),
     "hs_op_orthogonalize": (_I32, [_I32, _P, _P, _SZ, _P, _I32, _I32, _I32, _P, _D, _P, _SZ, _P]),
     "hs_muon_step": (_I32, [_P, _P, _P, _P, _SZ, _P, _I32, _I32, _D, _D, _D, _I32, _D, _D, _I32, _P, _D, _P, _SZ, _P]),
     "hs_cast_params": (_I32, [_P, _P, _SZ, _I32, _P]),
@@ -101,6 +102,7 @@ _SIGNATURES = {
     "hs_gemm_choice": (_I32, [_I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _SZ, C.POINTER(_I32), C.POINTER(_I32)]),
     "hs_op_gemm": (_I32, [_I32, _I32, _I32, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _I32, _F, _P, _I32, _P, _I64, _P, _P, _SZ, _P]),
     "hs_op_quantize_fp8": (_I32, [_I32, _P, _I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    "hs_gemm_fp8_choice": (_I32, [_I32, _I32, _I32, _I32, _SZ, C.POINTER(_I32), C.POINTER(_I32)]),
     "hs_op_gemm_fp8": (_I32, [_I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I32, _F, _P, _P, _SZ, _P]),
     "hs_op_layernorm_fwd": (_I32, [_I32, _P, _P, _P, _P, _P, _I32, _I32, _F, _P]),
     "hs_op_layernorm_bwd_scratch": (_SZ, [_I32, _I32]),
@@ -378,6 +380,13 @@ def hs_orthogonalize_workspace_bytes(mats, products) -> int:
     return n
 
 
+def hs_orthogonalize_choice(mats, products, matrix):
+    """(way, (sides of the tiles of X X^T, of a product of symmetric matrices, of S X)) of one matrix of a list."""
+    way, tiles = _I32(), (_I32 * 3)()
+    _check(lib().hs_orthogonalize_choice(mats, len(mats), products, matrix, C.byref(way), tiles))
+    return way.value, tuple(tiles)
+
+
 def _coeff(coeff, steps):
     """[steps, 3] coefficients as the host array that a call copies (None -> NULL)."""
     if coeff is None:
@@ -432,6 +441,13 @@ def hs_op_gemm_fp8(M, N, K, A, lda, a_scale, ldas, B, ldb, b_scale, ldbs, Cm, ld
                    stream=None):
     _check(lib().hs_op_gemm_fp8(M, N, K, _ptr(A), lda, _ptr(a_scale), ldas, _ptr(B), ldb, _ptr(b_scale), ldbs, _ptr(Cm), ldc, c_f32, beta, _ptr(bias),
                                 _ptr(scratch), scratch_bytes, _stream(stream)))
+
+
+def hs_gemm_fp8_choice(M, N, K, c_f32=0, scratch_bytes=0):
+    """(side of the tiles, number of splits) of an 8-bit product."""
+    tile, splits = _I32(), _I32()
+    _check(lib().hs_gemm_fp8_choice(M, N, K, c_f32, scratch_bytes, C.byref(tile), C.byref(splits)))
+    return tile.value, splits.value
 
 
 def hs_gemm_choice(a_kmajor, b_kmajor, M, N, K, c_f32=0, epi=0, a_padded=0, scratch_bytes=0):

@@ -356,6 +356,14 @@ void choose_fp8(int M, int N, int K, int c_f32, size_t scratch_bytes, int* cfg, 
   }
 }
 
+// The tile (its place in kFp8Cfg), the contraction of a part in whole scale words, and the parts that have some of it.
+void plan_fp8(int M, int N, int K, int c_f32, size_t scratch_bytes, int* cfg, int* k_per_split, int* splits) {
+  const int64_t kb = (K + (int64_t)127) / 128;
+  choose_fp8(M, N, K, c_f32, scratch_bytes, cfg, splits);
+  *k_per_split = std::max<int>(1, (int)((kb + *splits - 1) / *splits + 3) / 4) * 512;
+  *splits = std::max(1, (K + *k_per_split - 1) / *k_per_split);
+}
+
 }  // namespace
 
 extern "C" {
@@ -383,6 +391,14 @@ hs_status hs_op_quantize_fp8(int32_t dtype, const void* x, int64_t ldx, int32_t 
   return e == hipSuccess ? HS_OK : hs_fail(nullptr, HS_ERR_HIP, std::string("hs_op_quantize_fp8: ") + hipGetErrorString(e));
 }
 
+hs_status hs_gemm_fp8_choice(int32_t M, int32_t N, int32_t K, int32_t c_f32, size_t scratch_bytes, int32_t* tile, int32_t* splits) {
+  if (M < 1 || N < 1 || K < 1 || K > 1 << 22 || !tile || !splits) return hs_fail(nullptr, HS_ERR_INVALID_ARG, "hs_gemm_fp8_choice: bad argument");
+  int cfg, per, n;
+  plan_fp8(M, N, K, c_f32 ? 1 : 0, scratch_bytes, &cfg, &per, &n);
+  *tile = kFp8Cfg[0][cfg].b; *splits = n;
+  return HS_OK;
+}
+
 hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, const uint8_t* as, int64_t ldas, const void* B, int64_t ldb,
                          const uint8_t* bs, int64_t ldbs, void* C, int64_t ldc, int32_t c_f32, float beta, const void* bias, void* scratch,
                          size_t scratch_bytes, void* stream) {
@@ -402,9 +418,7 @@ hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t
   p.lda = lda; p.ldb = ldb; p.ldc = ldc;
   p.M = M; p.N = N; p.K = K; p.c_f32 = c_f32 ? 1 : 0; p.beta = beta;
   int cfg, splits;
-  choose_fp8(M, N, K, p.c_f32, scratch ? scratch_bytes : 0, &cfg, &splits);
-  p.k_per_split = std::max<int>(1, (int)((kb + splits - 1) / splits + 3) / 4) * 512;
-  splits = std::max(1, (K + p.k_per_split - 1) / p.k_per_split);
+  plan_fp8(M, N, K, p.c_f32, scratch ? scratch_bytes : 0, &cfg, &p.k_per_split, &splits);
   const int64_t bt = kFp8Cfg[0][cfg].b, blocks = ((M + bt - 1) / bt) * ((N + bt - 1) / bt) * splits;
   if (blocks >= ((int64_t)1 << 32) / 512) return hs_fail(nullptr, HS_ERR_SHAPE, "hs_op_gemm_fp8: too many tiles");      // threads of one launch
   p.partial = splits > 1 ? (float*)scratch : nullptr;

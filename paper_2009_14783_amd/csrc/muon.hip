@@ -891,8 +891,9 @@ hipError_t launch_product(NsDev& d, const IO& io, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(C::NT), lds, s, d, io);
   return hipGetLastError();
 }
-template <int OP, class IO>
-hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
+// The side of the tiles that a launch takes.
+template <int OP>
+int product_tile(const NsDev& d) {
   // Rounds that the tiles of a size take on the chip (one 256 x 256 tile per CU, two of 128 x 128, three of 64 x 64) times what a round takes, as a share of one
   // of 256 x 256 tiles, from lists of 48 and 96 matrices of 1024 x 1024 and 1024 x 4096 (us with 256, 128, 64: GRAM 171, 189, 219; SYM 216, 211, 242; APPLY
   // 303, 335, 466).  256 x 256 tiles are not built for 32-bit products, nor taken by SYM.  A launch whose 32 x 32 tiles all have a CU takes
@@ -903,13 +904,21 @@ hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
     for (int i = 0; i < d.n; ++i) tiles += ns_tiles(d.job[i].g, OP, b, b);
     return (float)((tiles + slots - 1) / slots);
   };
-  int64_t t32 = 0;
-  for (int i = 0; i < d.n; ++i) t32 += ns_tiles(d.job[i].g, OP, 32, 32);
-  if (t32 <= kCUs) return d.split ? launch_product<Ns32, OP, true, IO>(d, io, s) : launch_product<Ns32, OP, false, IO>(d, io, s);
+  if (rounds(32, kCUs) <= 1.0f) return 32;
   const float t256 = rounds(256, kCUs), t128 = rounds(128, 2 * kCUs) * kRound128, t64 = rounds(64, 3 * kCUs) * kRound64;
-  if (d.split) return t128 <= t64 ? launch_product<Ns128, OP, true, IO>(d, io, s) : launch_product<Ns64, OP, true, IO>(d, io, s);
-  if constexpr (OP != NS_SYM) { if (t256 <= std::min(t128, t64)) return launch_product<Ns256, OP, false, IO>(d, io, s); }
-  return t128 <= t64 ? launch_product<Ns128, OP, false, IO>(d, io, s) : launch_product<Ns64, OP, false, IO>(d, io, s);
+  if (!d.split && OP != NS_SYM && t256 <= std::min(t128, t64)) return 256;
+  return t128 <= t64 ? 128 : 64;
+}
+template <int OP, class IO>
+hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
+  switch (product_tile<OP>(d)) {
+    case 32: return d.split ? launch_product<Ns32, OP, true, IO>(d, io, s) : launch_product<Ns32, OP, false, IO>(d, io, s);
+    case 64: return d.split ? launch_product<Ns64, OP, true, IO>(d, io, s) : launch_product<Ns64, OP, false, IO>(d, io, s);
+    case 128: return d.split ? launch_product<Ns128, OP, true, IO>(d, io, s) : launch_product<Ns128, OP, false, IO>(d, io, s);
+    default: break;
+  }
+  if constexpr (OP != NS_SYM) return launch_product<Ns256, OP, false, IO>(d, io, s);
+  return hipErrorInvalidValue;
 }
 
 // A matrix whose longer side is at least twice the shorter is better served by polynomials of A than by products with X: over up to three steps
@@ -983,6 +992,18 @@ NsPlan ns_plan(const hs_matrix* mats, int n, int split) {
   }
   p.total = off;
   return p;
+}
+
+// Groups that go the same way, in runs of as many as the jobs of a launch.
+std::vector<std::vector<NsGroup>> ns_runs(const NsPlan& plan, int kind) {
+  const size_t most = kind == NS_BY_GRAM ? kJobs / 2 : kJobs;      // two products of a group in one launch
+  std::vector<std::vector<NsGroup>> runs;
+  for (const NsGroup& g : plan.groups) {
+    if (g.kind != kind) continue;
+    if (runs.empty() || runs.back().size() == most) runs.emplace_back();
+    runs.back().push_back(g);
+  }
+  return runs;
 }
 
 bool ns_list_ok(const hs_matrix* mats, int32_t n, std::string* why) {
@@ -1161,18 +1182,9 @@ hs_status orthogonalize_checked(const char* who, const IO& io, size_t size, cons
   }
   std::vector<double> c(3 * steps);
   for (int k = 0; k < 3 * steps; ++k) c[k] = coeff ? coeff[k] : kDefaultCoeff[k % 3];
-  // runs of groups that go the same way, as many as the jobs of a launch
-  for (int kind : {NS_BY_STEP, NS_BY_GRAM, NS_BY_PANEL}) {
-    std::vector<NsGroup> now;
-    const size_t most = kind == NS_BY_GRAM ? kJobs / 2 : kJobs;      // two products of a group in one launch
-    for (size_t i = 0; i <= plan.groups.size() && e == hipSuccess; ++i) {
-      if (!now.empty() && (i == plan.groups.size() || now.size() == most)) {
-        e = ns_run(now, kind, split, ws, table, places, (double*)(ws + plan.partial), io, steps, c.data(), eps, s);
-        now.clear();
-      }
-      if (i < plan.groups.size() && plan.groups[i].kind == kind) now.push_back(plan.groups[i]);
-    }
-  }
+  for (int kind : {NS_BY_STEP, NS_BY_GRAM, NS_BY_PANEL})
+    for (const std::vector<NsGroup>& now : ns_runs(plan, kind))
+      if (e == hipSuccess) e = ns_run(now, kind, split, ws, table, places, (double*)(ws + plan.partial), io, steps, c.data(), eps, s);
   return e == hipSuccess ? HS_OK : hs_fail(nullptr, HS_ERR_HIP, name + hipGetErrorString(e));
 }
 
@@ -1202,6 +1214,33 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
   } catch (const std::bad_alloc&) {
     hs_fail(nullptr, HS_ERR_STATE, "hs_orthogonalize_workspace_bytes: out of host memory");
     return 0;
+  }
+}
+
+hs_status hs_orthogonalize_choice(const hs_matrix* mats, int32_t n, int32_t products, int32_t matrix, int32_t* way, int32_t* tiles) {
+  try {
+    std::string why;
+    if (products != HS_FP32 && products != HS_BF16) why = "products must be HS_FP32 or HS_BF16";
+    else if (!ns_list_ok(mats, n, &why)) ;
+    else if (matrix < 0 || matrix >= n || !way || !tiles) why = "no such matrix, or nowhere to write";
+    if (!why.empty()) return hs_fail(nullptr, HS_ERR_INVALID_ARG, "hs_orthogonalize_choice: " + why);
+    const NsPlan plan = ns_plan(mats, n, products == HS_FP32);
+    const int at = (int)(std::find(plan.order.begin(), plan.order.end(), matrix) - plan.order.begin());
+    for (int kind : {NS_BY_STEP, NS_BY_GRAM, NS_BY_PANEL})
+      for (const std::vector<NsGroup>& now : ns_runs(plan, kind)) {
+        if (std::none_of(now.begin(), now.end(), [&](const NsGroup& g) { return at >= g.first && at < g.first + g.count; })) continue;
+        NsDev d{};
+        d.split = products == HS_FP32;
+        for (const NsGroup& g : now) d.job[d.n++].g = g;
+        const bool panel = kind == NS_BY_PANEL;
+        *way = kind;
+        tiles[0] = panel ? 0 : product_tile<NS_GRAM>(d);
+        tiles[1] = panel ? 0 : product_tile<NS_SYM>(d);
+        tiles[2] = panel ? 0 : product_tile<NS_APPLY>(d);
+      }
+    return HS_OK;
+  } catch (const std::bad_alloc&) {
+    return hs_fail(nullptr, HS_ERR_STATE, "hs_orthogonalize_choice: out of host memory");
   }
 }
 
