@@ -329,11 +329,13 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
 /* y = orthogonalised x, matrix by matrix.  X = x / (|x|_F + eps) (zeros stay zeros), then `steps` times
  * X <- a X + (b A + c A A) X with A = X X^T on the shorter side: an odd polynomial of the singular values, (a, b, c) =
  * coeff[3 k .. 3 k + 2] in step k, or 3.4445, -4.7750, 2.0315 in all when coeff is NULL (five steps take singular values from
- * 0.005 to 1 times the largest into 0.7 .. 1.2).
- * dtype: element type of x and y (flat buffers of `size` elements, in which the list's matrices lie; y may be x; elements outside the matrices
- * are not touched).  mats, coeff: host, copied.  products: HS_FP32 for products as exact as in fp32, HS_BF16 for 16-bit products with 32-bit
- * sums (relative error 0.5 to 2e-3 per matrix); both take any dtype.  The same call gives the same bits; how a matrix is rounded depends on the list
- * it is in, whose sizes decide the kernels.  The polynomials must keep the singular values below 3.9 and the entries of b A + c A A below 60 in size.
+ * 0.0015 to 1 times |x|_F into 0.68 .. 1.21; smaller ones grow by up to 480).
+ * dtype: element type of x and y (flat buffers of `size` elements, in which the list's matrices lie; y may be x, but must not overlap it otherwise;
+ * elements outside the matrices are not touched).  mats, coeff: host, copied.  products: HS_FP32 for products as exact as in fp32, HS_BF16 for 16-bit
+ * products with 32-bit sums; both take any dtype.  Relative error per matrix of 16-bit products with the default coefficients: up to 2e-3, and up to 3e-3
+ * where the library goes through polynomials of A, which it does with long matrices (a side twice the other) in large lists
+ * (hs_orthogonalize_choice says where; the upper ends are matrices of a few strong directions with little beside them).  The same call gives the same
+ * bits; how a matrix is rounded depends on the list it is in, whose sizes decide the kernels.  The polynomials must keep the singular values below 3.9 and the entries of b A + c A A below 60 in size.
  * A matrix with a value that is not finite becomes NaN as a whole; the others do not see it. */
 hs_status hs_op_orthogonalize(int32_t dtype, const void* x, void* y, size_t size, const hs_matrix* mats, int32_t n, int32_t products,
                               int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);
@@ -347,7 +349,8 @@ hs_status hs_orthogonalize_choice(const hs_matrix* mats, int32_t n, int32_t prod
  * mean square of the update rms times lr whatever the shape (rms > 0; 0.2 goes with learning rates made for Adam), or
  * s = sqrt(max(1, rows / cols)) (rms == 0).
  * w, m (in/out), G (in; unlike in hs_normalize_adam_step not written) flat fp32 [size] dev, w_lowp_out [size] dev bfloat16 or NULL as in hs_adam_step.  What
- * lies outside the list's matrices is neither read nor written: update it with hs_normalize_adam_step. */
+ * lies outside the list's matrices is neither read nor written: update it with hs_normalize_adam_step.  m is the sum of the rule above, not Adam's mean
+ * (1 - beta1) times that: a matrix that goes over from one rule to the other, as from a checkpoint, starts from an m of zeros. */
 hs_status hs_muon_step(float* w, float* m, const float* G, void* w_lowp_out, size_t size, const hs_matrix* mats, int32_t n,
                        int32_t products, double denom, double lr, double momentum, int32_t nesterov, double weight_decay, double rms,
                        int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);
@@ -471,7 +474,7 @@ hs_status hs_op_gemm(int32_t dtype, int32_t a_kmajor, int32_t b_kmajor, int32_t 
 
 /* ---- products in 8-bit floating point -----------------------------------------------------------
  * Operands are codes of e4m3 (1 sign, 4 exponent, 3 significand bits, largest value 448, 0x7f NaN), one byte each, with one scale
- * for every 128 of the contraction of every row: byte e stands for 2^(e - 127).  A row of K codes takes ceil(K / 128) whole blocks of
+ * for every 128 of the contraction of every row: byte e stands for 2^(e - 127), 255 for NaN.  A row of K codes takes ceil(K / 128) whole blocks of
  * 128 bytes, zeros behind the last code; its scales take a byte per block, in rows of whole 4-byte words.  Row strides are in bytes.
  *
  * hs_op_quantize_fp8 writes operands: x [R, C] (dtype, row stride ldx elements) as q [R, ldq], qs [R, ldqs] for contractions along its
@@ -482,11 +485,14 @@ hs_status hs_op_gemm(int32_t dtype, int32_t a_kmajor, int32_t b_kmajor, int32_t 
  * block are not written.  y = x W^T takes q of x and q of W; dx = dy W takes q of dy and qt of W; dW = dy^T x takes qt of dy and qt of x. */
 hs_status hs_op_quantize_fp8(int32_t dtype, const void* x, int64_t ldx, int32_t R, int32_t C, int32_t tile, void* q, int64_t ldq,
                              uint8_t* qs, int64_t ldqs, void* qt, int64_t ldqt, uint8_t* qts, int64_t ldqts, void* stream);
-/* C[M,N] = sum_k A(m,k) B(n,k) of such operands, with 32-bit sums; C is float (c_f32 != 0; C = beta C + sum, beta == 0 does not read C) or
- * bfloat16; bias [N] bfloat16 or NULL.  Row strides of codes multiples of 128 and at most 4 MiB, of scales multiples of 4.  scratch (dev, may
+/* C[M,N] = sum_k A(m,k) B(n,k) of such operands; C is float (c_f32 != 0; C = beta C + sum, beta == 0 does not read C) or bfloat16 (beta
+ * ignored); bias [N] bfloat16 or NULL.  Float results are 32-bit sums throughout.  For bfloat16 results the matrix instruction adds the products of 8
+ * neighbours with no more than 13 bits below the leading one of the largest, in 32 bits from there on: ordinarily 1.4e-5 to 4e-5 of the result, a hundredth of
+ * its rounding, but up to 2^-9 of the sum of the products' sizes where large ones cancel (448 448 - 448 448 + 2 is 0); who needs those sums takes a
+ * float result.  Row strides of codes multiples of 128 and at most 4 MiB, of scales multiples of 4.  scratch (dev, may
  * be NULL) as in hs_op_gemm: with it, contractions of products with few tiles are split and the partial sums added in a fixed order.
  * For float results every code times its scale is held as a bfloat16: exact for scale bytes 3 .. 246, while 0 .. 2 round to its multiples of 2^-133 and
- * 247 on (values from 448 2^119 on) may become infinite; bfloat16 results take every scale byte. */
+ * 247 to 254 (values from 448 2^119 on) may become infinite; bfloat16 results take every scale byte. */
 hs_status hs_op_gemm_fp8(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, const uint8_t* as, int64_t ldas, const void* B,
                          int64_t ldb, const uint8_t* bs, int64_t ldbs, void* C, int64_t ldc, int32_t c_f32, float beta,
                          const void* bias, void* scratch, size_t scratch_bytes, void* stream);

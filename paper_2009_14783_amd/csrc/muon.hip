@@ -10,8 +10,9 @@
 // decided by what the polynomial amplifies: a direction with a small singular value grows by a = 3.4 in every step, and the rounding of the large ones
 // would grow with it.  So X is kept as the sum of two fp16 numbers (22 bits) and a X is formed from both, in 32 bits; only the product with S reads the
 // first alone, and S vanishes on the small directions.  The diagonal of S, whose rounding is of one sign in a whole row of X, is taken out
-// of it and applied in 32 bits too.  Relative error of the result (2-norm, CPU emulation): Gaussian 768 x 768 8e-4, 512 x 512 of rank 32 with 2 % noise 8e-4; with
-// X in one fp16 number and the diagonal left in 1.4e-3 and 2.4e-2; all in bf16 1.1e-2 and 1.9e-1.  32-bit products (HS_FP32) take the second numbers of both operands
+// of it and applied in 32 bits too.  Relative error of the result (2-norm, CPU emulation), step by step: Gaussian 768 x 768 8e-4, 512 x 512 of rank 32 with 2 % noise 8e-4; with
+// X in one fp16 number and the diagonal left in 1.4e-3 and 2.4e-2; all in bf16 1.1e-2 and 1.9e-1.  Step by step and through polynomials of A: 256 x 1024 Gaussian 7e-4, 8e-4; of rank 64 with
+// 5 % noise 1.9e-3, 3.1e-3; rank 1 with 2 % 2e-4, 2.6e-3; on the card, 450 x 1100 of rank 28 with 5 % 1.7e-3 through A, 652 x 900 of rank 40 step by step 7e-4.  32-bit products (HS_FP32) take the second numbers of both operands
 // along: three products hi hi + hi lo + lo hi as one contraction three times as long, error as in fp32.
 #include <algorithm>
 #include <cmath>
@@ -929,7 +930,7 @@ hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
 constexpr double kGramAlone = 1.5e10, kGramBeside = 8e10;
 
 // Whether a list goes through the panel kernel: up to 128 rows in every matrix, blocks for about one round of the chip, and not too much to read of each other's
-// parts of A (a matrix of P panels: P P m m floats in a step).  Whole list in us, with and without: 130 x 67 in 32 bits 70, 107; 64 x 64 42, 94; 16 of
+// parts of A (a matrix of P panels: P P m m floats in a step).  The borders are the largest lists that measured better; nothing between them and the next ones was.  Whole list in us, with and without: 130 x 67 in 32 bits 70, 107; 64 x 64 42, 94; 16 of
 // 64 x 1024 (64 MB) 77, 106, 64 of them 223, 142; 24 layers of hidden 64 (288 blocks) 89, 107, 48 of them 132, 122; of 128 rows, whose steps are longer: toy model
 // 113, 121 (9 MB); 16 of 128 x 256 (17 MB) 94, 99; 16 of 128 x 512 (67 MB) 127, 103.
 bool ns_small(const std::vector<NsGroup>& groups) {

@@ -17,7 +17,8 @@ from . import binding as hs
 class MatrixUpdate:
     """Which parameters hs_muon_step updates and which are left to Adam: the weights of the layers and of the masked-LM head's transform as matrices (of
     the fused query/key/value projections every H x H block by itself), embeddings, biases and LayerNorm parameters by Adam.  The momentum of a matrix
-    is its slice of the worker's first moment, so that a checkpoint holds it."""
+    is its slice of the worker's first moment, so that a checkpoint holds it.  It is the sum mu m + g, not Adam's mean of (1 - beta1) g: a run that
+    goes over from one to the other (a checkpoint without `muon` resumed with it, or back) clears the first moment of the matrices."""
 
     DEFAULTS = dict(momentum=0.95, nesterov=True, weight_decay=0.0, rms=0.2, steps=5, coeff=None, eps=1e-7)
 
