@@ -332,10 +332,11 @@ size_t hs_orthogonalize_workspace_bytes(const hs_matrix* mats, int32_t n, int32_
  * 0.0015 to 1 times |x|_F into 0.68 .. 1.21; smaller ones grow by up to 480).
  * dtype: element type of x and y (flat buffers of `size` elements, in which the list's matrices lie; y may be x, but must not overlap it otherwise;
  * elements outside the matrices are not touched).  mats, coeff: host, copied.  products: HS_FP32 for products as exact as in fp32, HS_BF16 for 16-bit
- * products with 32-bit sums; both take any dtype.  Relative error per matrix of 16-bit products with the default coefficients: up to 2e-3, and up to 3e-3
- * where the library goes through polynomials of A, which it does with long matrices (a side twice the other) in large lists
- * (hs_orthogonalize_choice says where; the upper ends are matrices of a few strong directions with little beside them).  The same call gives the same
- * bits; how a matrix is rounded depends on the list it is in, whose sizes decide the kernels.  The polynomials must keep the singular values below 3.9 and the entries of b A + c A A below 60 in size.
+ * products with 32-bit sums; both take any dtype.  Relative error per matrix of 16-bit products with the default
+ * coefficients: ordinarily 0.3e-3 to 2e-3, but more where one or a few strong directions have a flat rest beside them or none: count on 3e-3 with 512 rows (the
+ * shorter side) and more, 5e-3 with 200, 1e-2 with 64, 3e-2 with 16, 6e-2 with fewer, and on 1e-2 where the library goes through polynomials of A, which it does in large lists with matrices of
+ * 512 rows and more (rounded up to 64) whose one side is twice the other (hs_orthogonalize_choice says where).  The same call gives the same bits; how a matrix is
+ * rounded depends on the list it is in, whose sizes decide the kernels.  The polynomials must keep the singular values below 3.9 and the entries of b A + c A A below 60 in size.
  * A matrix with a value that is not finite becomes NaN as a whole; the others do not see it. */
 hs_status hs_op_orthogonalize(int32_t dtype, const void* x, void* y, size_t size, const hs_matrix* mats, int32_t n, int32_t products,
                               int32_t steps, const double* coeff, double eps, void* workspace, size_t workspace_bytes, void* stream);

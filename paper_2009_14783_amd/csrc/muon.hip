@@ -12,7 +12,7 @@
 // first alone, and S vanishes on the small directions.  The diagonal of S, whose rounding is of one sign in a whole row of X, is taken out
 // of it and applied in 32 bits too.  Relative error of the result (2-norm, CPU emulation), step by step: Gaussian 768 x 768 8e-4, 512 x 512 of rank 32 with 2 % noise 8e-4; with
 // X in one fp16 number and the diagonal left in 1.4e-3 and 2.4e-2; all in bf16 1.1e-2 and 1.9e-1.  Step by step and through polynomials of A: 256 x 1024 Gaussian 7e-4, 8e-4; of rank 64 with
-// 5 % noise 1.9e-3, 3.1e-3; rank 1 with 2 % 2e-4, 2.6e-3; on the card, 450 x 1100 of rank 28 with 5 % 1.7e-3 through A, 652 x 900 of rank 40 step by step 7e-4.  32-bit products (HS_FP32) take the second numbers of both operands
+// 5 % noise 1.9e-3, 3.1e-3; rank 1 with 2 % 2e-4, 2.6e-3 (why the second only goes with many rows: see kGramAlone).  32-bit products (HS_FP32) take the second numbers of both operands
 // along: three products hi hi + hi lo + lo hi as one contraction three times as long, error as in fp32.
 #include <algorithm>
 #include <cmath>
@@ -922,12 +922,18 @@ hipError_t product(NsDev& d, const IO& io, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
-// A matrix whose longer side is at least twice the shorter is better served by polynomials of A than by products with X: over up to three steps
+// A large matrix whose longer side is at least twice the shorter is better served by polynomials of A than by products with X: over up to three steps
 // X <- S_3 S_2 S_1 X with S_i = a I + b A_i + c A_i A_i and A_(i+1) = S_i A_i S_i, all symmetric m x m matrices that commute, and X itself is read
 // and written once.  Five steps are 6 m m n + 14 m m m operations instead of 15 m m n + 5 m m m, in 17 launches instead of 15, beside those of the matrices that stay with the
-// other form.  Where that pays (us, with and without): of a list by itself from 1.5e10 operations saved on (16 of 256 x 2048: 179, 191; 4: 156, 147), in a
-// stack of layers with square matrices from 8e10 on (12 layers of hidden 512: 1037, 1082; 3 of 768: 723, 699; 24 of 1024: 8.6 ms, 10.1 ms).
+// other form.  Where that pays (us, with and without, over 60 lists): of a list by itself from 1.5e10 operations saved on (2 of 640 x 2560, 1.4e10: 212, 228; 4 of 768 x 1536, 1.6e10: 251, 247;
+// 12 of 1024 x 4096: 1169, 1586), in a stack of layers with square matrices from 8e10 on (12 layers of hidden 512, 8.7e10: 1048, 1204; 3 of 768, 7.3e10: 766, 743; 8 of 1024 with matrices 1 : 2,
+// 1.5e11, the worst: 2581, 2442; 24 of 1024: 8.3 ms, 9.6 ms).
+// From 512 rows on: A is not formed from X again in between, so that the rounding that its strong directions make stays in its weak ones, which grow by a in every step; it is the
+// smaller the more rows it is spread over.  The worst of 80 spectra, one strong direction and a flat rest, came out 3.1e-2 off with 64 rows, 2.2e-2 with 128, 1.3e-2 with 256, 7e-3 with 512 and 5e-3 with
+// 1024; step by step 7.5e-3, 4.0e-3, 2.8e-3, 1.7e-3 and 1.4e-3.
 constexpr double kGramAlone = 1.5e10, kGramBeside = 8e10;
+constexpr int kGramRows = 512;
+bool ns_long(const NsGroup& g) { return g.m >= kGramRows && g.n >= 2 * g.m; }
 
 // Whether a list goes through the panel kernel: up to 128 rows in every matrix, blocks for about one round of the chip, and not too much to read of each other's
 // parts of A (a matrix of P panels: P P m m floats in a step).  The borders are the largest lists that measured better; nothing between them and the next ones was.  Whole list in us, with and without: 130 x 67 in 32 bits 70, 107; 64 x 64 42, 94; 16 of
@@ -980,12 +986,12 @@ NsPlan ns_plan(const hs_matrix* mats, int n, int split) {
   double saved = 0.0;
   bool others = false;
   for (const NsGroup& g : p.groups) {
-    if (!split && g.n >= 2 * g.m) saved += 9.0 * g.m * (double)g.m * (g.n - g.m) * g.count;
+    if (!split && ns_long(g)) saved += 9.0 * g.m * (double)g.m * (g.n - g.m) * g.count;
     else others = true;
   }
   const bool gram = saved >= (others ? kGramBeside : kGramAlone);
   for (NsGroup& g : p.groups) {
-    g.kind = small ? NS_BY_PANEL : gram && g.n >= 2 * g.m ? NS_BY_GRAM : NS_BY_STEP;
+    g.kind = small ? NS_BY_PANEL : gram && ns_long(g) ? NS_BY_GRAM : NS_BY_STEP;
     if (small) g.m = (std::min(g.rows, g.cols) + 31) / 32 * 32;
     g.bufs = g.kind == NS_BY_GRAM ? BUFS : BUF_S + 1;
     g.ws = (int64_t)off; g.stride = (int64_t)matrix_bytes(g, split);

@@ -63,8 +63,8 @@ def test_nan_stays_in_its_row_and_column_of_large_tiles(hs):
 # ---- matrices -------------------------------------------------------------------------------------------
 # (products, shape, count, way, sides of the tiles of X X^T, of symmetric products, of S X)
 LISTS = [(1, (300, 300), 58, 0, (64, 128, 64)), (1, (330, 330), 76, 0, (128, 128, 128)), (1, (430, 430), 85, 0, (256, 128, 128)),
-         (1, (652, 900), 37, 0, (256, 128, 256)), (1, (900, 652), 37, 0, (256, 128, 256)), (1, (450, 1100), 17, 1, (64, 64, 256)),
-         (1, (330, 900), 74, 1, (128, 128, 128)), (1, (1100, 450), 72, 1, (256, 128, 256)),
+         (1, (652, 900), 37, 0, (256, 128, 256)), (1, (900, 652), 37, 0, (256, 128, 256)), (1, (600, 1300), 11, 1, (64, 64, 256)),
+         (1, (600, 1300), 29, 1, (128, 128, 128)), (1, (1500, 650), 36, 1, (256, 128, 256)),
          (0, (330, 330), 22, 0, (64, 64, 128)), (0, (330, 330), 76, 0, (128, 128, 128)), (0, (652, 900), 37, 0, (64, 128, 128)),
          (0, (900, 652), 37, 0, (64, 128, 128))]
 

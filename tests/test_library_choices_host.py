@@ -32,6 +32,7 @@ def test_lists_of_matrices():
     assert hs.hs_orthogonalize_choice(stack([(100, 300)]), 1, 0) == (2, (0, 0, 0))
     mixed = stack([(1024, 1024)] * 96 + [(4096, 1024), (1024, 4096)] * 24)
     assert [hs.hs_orthogonalize_choice(mixed, 1, i)[0] for i in (0, 95, 96, 143)] == [0, 0, 1, 1]
+    assert hs.hs_orthogonalize_choice(stack([(64, 4000)] * 200), 1, 0)[0] == 0      # nor are few rows taken through A alone
     assert hs.hs_orthogonalize_choice(mixed, 0, 143)[0] == 0                     # 32-bit products go step by step
     for products in (0, 1):
         for shapes in ([(130, 190)], [(330, 330)] * 40, [(200, 2000)] * 100, [(64 + i, 400) for i in range(40)]):
