@@ -601,7 +601,7 @@ void ns_product_kernel(NsDev d, IO io) {
 // ---- small matrices ---------------------------------------------------------------------------------
 // With up to 128 rows all of A and S fits the LDS of a CU, and S takes it less time than a launch: every block forms S for itself and applies it to 64 columns
 // of X, which it then multiplies with themselves for its part of the next A.  One launch per step instead of three, rows padded to multiples of 32; the
-// blocks of a matrix add up each other's parts of A in their order.  What bounds it is latency, about 6 us a step with 64 rows and 11 with 128: one block of 512 threads
+// blocks of a matrix add up each other's parts of A in their order.  What bounds it is latency, 7 us a step with 64 rows, 10 with 96 and 13 to 18 with 128: one block of 512 threads
 // per CU.  Which lists go this way: ns_small.
 enum { PANEL_FIRST = 0, PANEL_STEP, PANEL_LAST };
 constexpr int kPanelThreads = 512, kPanelM = 128;
